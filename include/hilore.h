@@ -18,6 +18,10 @@
  *   susceptibility kappa_c and mean reconstruction error     -> hilore_calibrate
  *   psi_u = kappa E_u ebar_u, the risk input of Allocate     -> hilore_risk_score
  * Diagnostics (App. D.3): zero-gradient causes, top-k share  -> hilore_update_sparsity
+ * Around them, the layer that recomputes, consumes and trains what the units hold:
+ *   norms on leaving a block and entering the next, and back -> hilore_block_norm, hilore_block_norm_bwd
+ *   frozen base weights in int8, forward and input gradient  -> hilore_int8_linear, hilore_int8_matmul
+ *   optimizer step on the gradients, and their global norm   -> hilore_adamw, hilore_grad_norm
  *
  * Conventions shared by every entry point:
  *   - Every tensor pointer is a DEVICE pointer owned by the caller.  The
@@ -33,8 +37,9 @@
  *     device state, so argument errors are reported even without a GPU.
  *   - bf16 tensors are passed as uint16_t* (raw bit patterns).
  *   - Alignment: every tensor pointer must be 16-byte aligned, except the
- *     per-unit outputs of hilore_unit_exposure_risk (4-byte aligned) and the
- *     per-unit arrays of hilore_allocate (8-byte aligned for fp64).
+ *     per-unit outputs of hilore_unit_exposure_risk (4-byte aligned), the
+ *     per-unit arrays of hilore_allocate (8-byte aligned for fp64) and the
+ *     scales of 8-bit optimizer states (4-byte aligned).
  *   - The functions are re-entrant; calls on different streams may run
  *     concurrently.  No C++ exception crosses this interface.
  *   - Results do not depend on the launch configuration: every reduction is
@@ -447,6 +452,242 @@ hilore_status hilore_risk_score(int n_units, const int32_t *unit_class, int n_cl
 hilore_status hilore_update_sparsity(const float *coeff, const uint8_t *flags, const float *adv,
                                      const uint8_t *mask, int R, int T, double top_frac,
                                      int64_t *counts, double *top_share, void *stream);
+
+/* How the gate of hilore_block_norm is broadcast over a [rows, cols] block output. */
+typedef enum hilore_gate {
+  HILORE_GATE_NONE = 0,
+  HILORE_GATE_CHANNEL = 1, /* bf16 [cols]: a learned scale of every channel      */
+  HILORE_GATE_TOKEN = 2,   /* bf16 [rows]: one value a token, e.g. of a router   */
+  HILORE_GATE_ELEMENT = 3  /* bf16 [rows, cols] dense: one value an element      */
+} hilore_gate;
+
+/*
+ * Leaving a block and entering the next: the norm of the block's output y, its
+ * gate, the residual sum with a scale, and the norm before the next block, in one
+ * pass over the rows.  With N(v) = v * rsqrt(mean(v^2) + eps) over a row:
+ *   h = bf16_RNE(res + scale * gate * (N(y) * w_post))
+ *   n = N(h) * w_pre          of h as it is stored, so that a recompute from a kept
+ *                             h gives the same n bit for bit
+ *   res      bf16 [rows, cols], row stride ld_res (>= cols, % 8 == 0)
+ *   y        bf16 [rows, cols], row stride ld_y; NULL: no block output (the norm
+ *            before a model's first block): h = res, and w_post and gate must be NULL
+ *   w_post   bf16 [cols]; NULL: y enters without a norm
+ *   gate     by gate_kind; NULL with HILORE_GATE_NONE
+ *   w_pre    bf16 [cols]; NULL: no norm before a next block (then no n, codes, rstd_pre)
+ * Outputs, each but one of h, n and codes may be NULL:
+ *   h        bf16 [rows, cols] dense; may be res itself where ld_res == cols
+ *   n        bf16 [rows, cols] dense
+ *   codes    int8 [rows, cols] dense, with code_scales f32 [rows]: n rounded token by
+ *            token as hilore_int8_linear rounds its operand (from the fp32 n, not from
+ *            its bf16 value), the operand of hilore_int8_matmul
+ *   rstd_post, rstd_pre  f32 [rows]: the rsqrt factors of N(y) and N(h), for backward
+ * fp32 arithmetic, row sums in a fixed order.  Limits: cols % 8 == 0 (with codes %
+ * 16 == 0), cols <= 16384, rows < 2^31.
+ */
+typedef struct hilore_block_norm_desc {
+  const uint16_t *res;
+  const uint16_t *y;
+  const uint16_t *w_post;
+  const uint16_t *gate;
+  const uint16_t *w_pre;
+  uint16_t *h;
+  uint16_t *n;
+  int8_t *codes;
+  float *code_scales;
+  float *rstd_post;
+  float *rstd_pre;
+  int64_t rows;
+  int64_t cols;
+  int64_t ld_res;
+  int64_t ld_y;
+  float scale;
+  float eps;
+  int gate_kind;
+} hilore_block_norm_desc;
+hilore_status hilore_block_norm(const hilore_block_norm_desc *d, void *stream);
+
+/*
+ * Backward of hilore_block_norm.  With hh = h * rstd_pre, yh = y * rstd_post, means
+ * and sums over a row's columns:
+ *   D    = dh + rstd_pre * (dn * w_pre - hh * mean(dn * w_pre * hh))
+ *   dres = D,   z = yh * w_post,   dz = scale * gate * D
+ *   dy   = rstd_post * (dz * w_post - yh * mean(dz * w_post * yh))   (dz without w_post)
+ *   dw_pre = sum_rows dn * hh,   dw_post = sum_rows dz * yh,
+ *   dgate  = scale * D * z, summed over what the gate was broadcast over
+ *   h, y     the saved tensors as units: codes (+ scales) for an L unit, decoded in
+ *            registers to the bf16 value hilore_decompress writes; otherwise x, bf16
+ *            with row stride ld.  Either may be L (then with the same code and block).
+ *            h is read only with dn; y (rows, cols of all zero: none) only with w_post
+ *            or a dgate
+ *   dn       bf16 [rows, cols], row stride ld_dn, the gradient of n; NULL: none (then
+ *            w_pre, rstd_pre, dw_pre must be NULL)
+ *   dh       bf16 [rows, cols] dense, the gradient that reaches h past the next block;
+ *            NULL: none
+ * Outputs, each may be NULL (frozen weights take no dw_*, no dgate of a channel):
+ *   dres, dy bf16 [rows, cols] dense; dres may be dh itself
+ *   dw_pre, dw_post f32 [cols]; dgate f32 [cols], f32 [rows] or bf16 [rows, cols] by
+ *   gate_kind.  accumulate != 0 adds dw_pre, dw_post and a channel's dgate to what is
+ *   there; all other outputs are overwritten.
+ * fp32 arithmetic; the sums over rows go to `workspace` by workgroups and are added in
+ * a fixed order (no floating-point atomics).  workspace: device memory of at least
+ * hilore_block_norm_bwd_workspace_bytes(d) bytes (0, and then NULL is allowed, without
+ * sums over rows), 16-byte aligned, contents on entry irrelevant; calls sharing it must
+ * not overlap.  Limits as for hilore_block_norm; with L units cols % block == 0.
+ */
+typedef struct hilore_block_norm_bwd_desc {
+  hilore_unit_desc h;
+  hilore_unit_desc y;
+  const uint16_t *w_post;
+  const uint16_t *gate;
+  const uint16_t *w_pre;
+  const float *rstd_post;
+  const float *rstd_pre;
+  const uint16_t *dn;
+  const uint16_t *dh;
+  uint16_t *dres;
+  uint16_t *dy;
+  float *dw_post;
+  float *dw_pre;
+  void *dgate;
+  int64_t rows;
+  int64_t cols;
+  int64_t ld_dn;
+  float scale;
+  int gate_kind;
+} hilore_block_norm_bwd_desc;
+size_t hilore_block_norm_bwd_workspace_bytes(const hilore_block_norm_bwd_desc *d);
+hilore_status hilore_block_norm_bwd(const hilore_block_norm_bwd_desc *d, int code, int block,
+                                    int accumulate, void *workspace, size_t workspace_bytes,
+                                    void *stream);
+
+/*
+ * Linear layer with int8 weights of one scale per output channel (the frozen base
+ * weights of the adapter setting, App. D.1.1), its operand rounded to int8 with one
+ * scale per token:
+ *   a[t][k] = RNE(x'[t][k] * (127 / amax_t)) clamped to [-127, 127],  sa_t = amax_t / 127,
+ *             x' = x * factor (fp32), amax_t = max_k |x'[t][k]|  (IEEE fp32 quotients;
+ *             amax_t < 2^-64: codes and sa_t are 0; not finite: codes 0, sa_t NaN)
+ *   out[t][n] (+)= (sum_k a[t][k] * w[n][k]) * sa_t * sw_n + bias[n]
+ * The sums are exact in int32 (k <= 131072); the rest is fp32 in that order, rounded
+ * once to the output's type.
+ *   x        bf16 [tokens, k], row stride ldx (>= k, % 8 == 0); factor f32 [k] or NULL
+ *   a        int8 [tokens, k] dense with a_scales f32 [tokens]: codes in hand, for
+ *            hilore_int8_matmul (x, ldx and factor are not read)
+ *   w        int8 [n, k] dense, values in [-127, 127]; w_scales f32 [n], or NULL: 1
+ *   bias     bf16 [n] or NULL
+ *   out      bf16 or (out_f32 != 0) f32 [tokens, n], row stride ldo (>= n, % 8 == 0);
+ *            accumulate != 0 adds to it (in fp32, rounded once)
+ * Gradient of the layer's input, dX = (dY * sw) W: hilore_int8_linear with x = dY,
+ * factor = w_scales of the layer, w = the layer's codes transposed (once) to [k, n],
+ * and no w_scales.  Several layers on one input add up with accumulate.
+ * hilore_quantize_tokens is the rounding alone; with a weight [n, k] as x it makes
+ * the weight's codes and channel scales.
+ * workspace: device memory of at least hilore_int8_workspace_bytes(d, quantize) bytes
+ * (quantize: 1 for hilore_int8_linear, 0 for hilore_int8_matmul; 0 bytes, and then NULL
+ * is allowed, where none is needed), 16-byte aligned, contents on entry irrelevant;
+ * calls sharing it must not overlap.
+ * Limits: k % 16 == 0, n % 8 == 0, k <= 131072, n < 2^26, tokens < 2^31 (else
+ * UNSUPPORTED); k = 0 writes bias or zeros.
+ */
+typedef struct hilore_int8_desc {
+  const uint16_t *x;
+  const float *factor;
+  const int8_t *a;
+  const float *a_scales;
+  const int8_t *w;
+  const float *w_scales;
+  const uint16_t *bias;
+  void *out;
+  int64_t tokens;
+  int64_t k;
+  int64_t n;
+  int64_t ldx;
+  int64_t ldo;
+  int out_f32;
+  int accumulate;
+} hilore_int8_desc;
+size_t hilore_int8_workspace_bytes(const hilore_int8_desc *d, int quantize);
+hilore_status hilore_int8_linear(const hilore_int8_desc *d, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+hilore_status hilore_int8_matmul(const hilore_int8_desc *d, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+hilore_status hilore_quantize_tokens(const uint16_t *x, const float *factor, int64_t tokens,
+                                     int64_t k, int64_t ldx, int8_t *codes, float *scales,
+                                     void *stream);
+
+/*
+ * One tensor of an optimizer step, its gradient and its states.
+ *   p        f32 [n] parameters, or NULL; p16 bf16 [n] or NULL.  Both: p is the
+ *            parameter and p16 receives its nearest bf16.  p16 alone: the parameter is
+ *            bf16 and the new value is rounded up or down at random (below), so that
+ *            steps smaller than half a bf16 spacing are not lost
+ *   grad     f32 [n], or bf16 [n] with grad_bf16 != 0
+ *   m, v     states in 32 bits (m_scales and v_scales NULL): f32 [n], the running means
+ *            of g and g^2.  In 8 bits: E4M3FN codes [n] with f32 [ceil(n / 256)] scales
+ *            of m and of r = sqrt(v), value = value(code) * scale (scales 4-byte aligned:
+ *            those of many tensors may lie one after another)
+ *   lr, weight_decay  of this tensor (its parameter group)
+ */
+typedef struct hilore_adamw_tensor {
+  float *p;
+  uint16_t *p16;
+  const void *grad;
+  void *m;
+  void *v;
+  float *m_scales;
+  float *v_scales;
+  int64_t n;
+  float lr;
+  float weight_decay;
+  int grad_bf16;
+} hilore_adamw_tensor;
+
+/*
+ * Global norm of the gradients of many tensors and the factor that clips it:
+ *   norm[0] = sqrt(sum over all tensors of g^2),
+ *   norm[1] = min(1, max_norm / (norm[0] + 1e-6)), or 1 where max_norm is infinite;
+ *             NaN where norm[0] is not finite (hilore_adamw then leaves everything as it is)
+ * tensors[n_tensors] is a host array, read during the call; uses grad, grad_bf16, n.
+ * norm f32 [2] on the device, 4-byte aligned.  fp64 sums in a fixed order, rounded to
+ * fp32's 24 bits; root, sum and quotient are IEEE fp32 operations on that.
+ * workspace: device memory of at least hilore_grad_norm_workspace_bytes(tensors,
+ * n_tensors) bytes, 16-byte aligned, contents on entry irrelevant; calls sharing it
+ * must not overlap.  Errors: max_norm not positive, null pointers, negative sizes ->
+ * INVALID_ARG; over 2^40 elements in all -> UNSUPPORTED; workspace too small -> WORKSPACE.
+ */
+size_t hilore_grad_norm_workspace_bytes(const hilore_adamw_tensor *tensors, int n_tensors);
+hilore_status hilore_grad_norm(const hilore_adamw_tensor *tensors, int n_tensors, double max_norm,
+                               float *norm, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+/*
+ * One AdamW step (decoupled weight decay) over many tensors, g = grad * norm[1]:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * fp32 arithmetic; the update uses the new states before their rounding.
+ *   norm     f32 [2] of hilore_grad_norm, or NULL: g = grad.  Where norm[1] is NaN
+ *            nothing is written (a step with an infinite or NaN gradient is skipped)
+ *   step     1 for the first step
+ *   seed     of the random rounding; give each step its own
+ * 8-bit states: per 256 elements scale = amax * (1/448) (0 where amax < 2^-64, as the
+ * codec's), codes of |value| * (448 * (1/amax)), and a value between two codes takes the upper one with the probability of
+ * its place between them, so that the rounding is unbiased and changes far below a
+ * code's spacing, as (1 - beta2) makes them, add up over steps instead of vanishing.
+ * r > 0 never becomes code 0: a lost second moment would leave eps alone under m.
+ * Random bits: 32 per element, R = mix(i ^ K), K = mix(seed + 0x9E3779B1 (tensor + 1) + salt)
+ * in 32-bit arithmetic with i the element's index (below 2^32) in tensor `tensor` of the
+ * call, mix(x): x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xBB67AE85, x ^= x >> 16.
+ * Salt 0: low half for m, high half for r, as the 16 bits below the code; salt
+ * 0x3C6EF372: low half as the 16 bits below a bf16 parameter.  The same inputs and seed
+ * give the same bits in every call.
+ * All tensors may differ in every field; all are done by ceil(n_tensors / 44) launches.
+ * Limits: n < 2^32 for a tensor (else UNSUPPORTED).  Errors: betas outside [0, 1), eps not
+ * a positive normal float, step < 1, null pointers, negative sizes, lr or weight_decay not
+ * finite, one of m_scales and v_scales alone -> INVALID_ARG.
+ */
+hilore_status hilore_adamw(const hilore_adamw_tensor *tensors, int n_tensors, double beta1,
+                           double beta2, double eps, int64_t step, const float *norm,
+                           uint32_t seed, void *stream);
 
 #ifdef __cplusplus
 }

@@ -8,31 +8,13 @@
 #include <cmath>
 #include <cstdint>
 
+#include "abi_common.hpp"
 #include "hilore_internal.hpp"
 
 namespace {
 
 using hilore::CodecBatch;
 using hilore::CodecUnit;
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-bool valid_block(int block) { return block == 32 || block == 64 || block == 128 || block == 256; }
-
-bool valid_code(int code) {
-  return code == HILORE_CODE_INT8 || code == HILORE_CODE_FP8_E4M3FN ||
-         code == HILORE_CODE_FP8_E4M3FN_CAST;
-}
-
-// The blockwise codes need a supported block size; the literal cast has no
-// blocks and takes block == 0.
-hilore_status check_code_block(int code, int block) {
-  if (!valid_code(code)) return HILORE_ERR_INVALID_ARG;
-  if (code == HILORE_CODE_FP8_E4M3FN_CAST) return block == 0 ? HILORE_OK : HILORE_ERR_INVALID_ARG;
-  return valid_block(block) ? HILORE_OK : HILORE_ERR_UNSUPPORTED;
-}
-
-hilore_status hip_status(hipError_t e) { return e == hipSuccess ? HILORE_OK : HILORE_ERR_HIP; }
 
 // Check the fields of one unit that an entry point reads.
 enum UnitUse : unsigned {

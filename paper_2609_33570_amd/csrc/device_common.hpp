@@ -24,6 +24,50 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
+// The 8 bf16 values of w as fp32 (exact).
+__device__ __forceinline__ void unpack_bf16x8(u32x4 w, float v[8]) {
+  v[0] = bf16_lo(w.x); v[1] = bf16_hi(w.x);
+  v[2] = bf16_lo(w.y); v[3] = bf16_hi(w.y);
+  v[4] = bf16_lo(w.z); v[5] = bf16_hi(w.z);
+  v[6] = bf16_lo(w.w); v[7] = bf16_hi(w.w);
+}
+
+__device__ __forceinline__ u32x4 pack_bf16x8(const float v[8]) {
+  return u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]),
+               pack_bf16(v[6], v[7])};
+}
+
+// 8 codes of an L unit as the bf16 values that decompress writes, in fp32
+// (SCALED: times their block scale s and rounded; else exact values of the cast).
+template <bool INT8, bool SCALED>
+__device__ __forceinline__ void decode_codes8(u32x2 c, float s, float v[8]) {
+  float q[8];
+  if constexpr (INT8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      q[i] = (float)(int)__builtin_amdgcn_sbfe(c.x, 8 * i, 8);
+      q[4 + i] = (float)(int)__builtin_amdgcn_sbfe(c.y, 8 * i, 8);
+    }
+  } else {
+    f32x2 d;
+    d = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.x, false); q[0] = d.x; q[1] = d.y;
+    d = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.x, true);  q[2] = d.x; q[3] = d.y;
+    d = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.y, false); q[4] = d.x; q[5] = d.y;
+    d = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.y, true);  q[6] = d.x; q[7] = d.y;
+  }
+  if constexpr (SCALED) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const uint32_t h = pack_bf16(q[i] * s, q[i + 1] * s);
+      v[i] = bf16_lo(h);
+      v[i + 1] = bf16_hi(h);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = q[i];
+  }
+}
+
 // Cross-lane operations inside a wave.  DPP controls (gfx9 encoding).
 enum : int {
   kDppQuadXor1 = 0xB1,      // quad_perm [1,0,3,2]
@@ -76,6 +120,32 @@ __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) v += __shfl_xor(v, off, kWave);
   return v;
+}
+
+// Rounding of a token's values to int8: the factor 127 / amax and the scale amax / 127.
+// Below 2^-64 both are 0; an infinite or NaN amax gives factor 0 and scale NaN.
+__device__ __forceinline__ float token_scale(float amax, float &scale) {
+  if (amax < 0x1p-64f) {
+    scale = 0.0f;
+    return 0.0f;
+  }
+  if (!(amax < __builtin_inff())) {
+    scale = __builtin_nanf("");
+    return 0.0f;
+  }
+  scale = amax / 127.0f;
+  return 127.0f / amax;
+}
+
+// 8 codes RNE(v * r), clamped to [-127, 127]; 0 where r is 0 (v may be anything then).
+__device__ __forceinline__ u32x2 token_codes8(const float v[8], float r) {
+  uint32_t c[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float q = __builtin_amdgcn_fmed3f(rintf(v[i] * r), -127.0f, 127.0f);
+    c[i] = r == 0.0f ? 0u : (uint32_t)(int)q & 0xFFu;
+  }
+  return u32x2{c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24};
 }
 
 }  // namespace hilore

@@ -276,4 +276,113 @@ struct SwigluArgs {
 };
 hipError_t launch_swiglu_bwd(const SwigluArgs &a, int code, int block, hipStream_t s);
 
+// AdamW and the gradients' global norm.  The tensors of one launch travel by value
+// in the kernel arguments (4 KB at most); workgroups are numbered through them in
+// chunks.
+constexpr int kAdamwBlock = 256;          // elements per scale of an 8-bit state
+constexpr int64_t kAdamwChunk = 4096;     // elements per workgroup
+constexpr int kAdamwPerLaunch = 44;
+struct AdamwTensor {
+  float *p;
+  uint16_t *p16;
+  const void *grad;
+  void *m, *v;
+  float *m_scales, *v_scales;
+  int64_t n;
+  float step_size, decay;  // lr / (1 - beta1^step), 1 - lr * weight_decay
+  uint32_t key_state, key_param;
+  int grad16;
+};
+struct AdamwBatch {
+  AdamwTensor t[kAdamwPerLaunch];
+  uint32_t begin[kAdamwPerLaunch + 1];  // prefix sum of the tensors' chunks
+  int n;
+  const float *norm;
+  float beta1, one_beta1, beta2, one_beta2, eps, inv_sqrt_c2;
+};
+static_assert(sizeof(AdamwBatch) <= 4096, "kernel arguments");
+hipError_t launch_adamw(const AdamwBatch &a, hipStream_t s);
+uint32_t adamw_key(uint32_t seed, int index, uint32_t salt);
+
+constexpr int64_t kNormChunk = 16384;     // elements per workgroup
+constexpr int kNormPerLaunch = 128;
+struct NormTensor {
+  const void *grad;
+  int64_t n;
+  int64_t grad16;
+};
+struct NormBatch {
+  NormTensor t[kNormPerLaunch];
+  uint32_t begin[kNormPerLaunch + 1];
+  int n;
+  double *part;  // partial sums of this launch's chunks
+};
+static_assert(sizeof(NormBatch) <= 4096, "kernel arguments");
+hipError_t launch_norm_partial(const NormBatch &a, hipStream_t s);
+hipError_t launch_norm_fold(const double *part, int64_t n, float max_norm, float *norm,
+                            hipStream_t s);
+
+// Norms around a block.
+constexpr int64_t kNormMaxCols = 16384;
+struct BlockNormArgs {
+  const uint16_t *res, *y, *w_post, *gate, *w_pre;
+  uint16_t *h, *n;
+  int8_t *codes;
+  float *code_scales, *rstd_post, *rstd_pre;
+  int64_t rows, ld_res, ld_y;
+  int cols;
+  float scale, eps, inv_cols;
+  int gate_kind;
+};
+hipError_t launch_block_norm(const BlockNormArgs &a, hipStream_t s);
+
+struct SavedRows {  // a saved tensor: bf16 rows x, or codes with scales
+  const uint16_t *x;
+  const uint8_t *codes;
+  const float *scales;
+  int64_t ld;
+};
+struct BlockNormBwdArgs {
+  SavedRows h, y;
+  const uint16_t *w_post, *gate, *w_pre, *dn, *dh;
+  const float *rstd_post, *rstd_pre;
+  uint16_t *dres, *dy;
+  float *dw_post, *dw_pre;
+  void *dgate;
+  int64_t rows, ld_dn;
+  int cols;
+  float scale, inv_cols;
+  int gate_kind, accumulate;
+  int code, block_log2;  // of L units
+  int sums;              // sums over rows wanted (dw_pre, dw_post, a channel's dgate)
+  int groups;            // workgroups
+  float *part;           // workspace: [sum][workgroup][cols]
+};
+int block_norm_bwd_groups(int64_t rows, int64_t cols, int sums);
+hipError_t launch_block_norm_bwd(const BlockNormBwdArgs &a, hipStream_t s);
+
+// int8 products.
+struct QuantArgs {
+  const uint16_t *x;
+  const float *factor;
+  int8_t *codes;
+  float *scales;
+  int64_t tokens, k, ldx;
+};
+hipError_t launch_quantize_tokens(const QuantArgs &a, hipStream_t s);
+
+struct Int8Args {
+  const int8_t *a, *w;
+  const float *a_scales, *w_scales;
+  const uint16_t *bias;
+  void *out;
+  int64_t tokens, n, ldo;
+  int k;
+  int out_f32, accumulate;
+  int32_t *part;  // workspace
+};
+constexpr int64_t kInt8MaxK = 131072;  // 2^17 * 127^2 < 2^31
+size_t int8_part_bytes(int64_t tokens, int64_t k, int64_t n);
+hipError_t launch_int8(const Int8Args &a, hipStream_t s);
+
 }  // namespace hilore

@@ -53,38 +53,8 @@ __device__ __forceinline__ void load_operand(const uint16_t *x, const uint8_t *c
 // The 8 values as fp32: an L operand decoded exactly as decompress does it.
 template <int CODE, bool L>
 __device__ __forceinline__ void decode_operand(const Raw &r, float v[8]) {
-  if constexpr (!L) {
-    v[0] = bf16_lo(r.w.x); v[1] = bf16_hi(r.w.x);
-    v[2] = bf16_lo(r.w.y); v[3] = bf16_hi(r.w.y);
-    v[4] = bf16_lo(r.w.z); v[5] = bf16_hi(r.w.z);
-    v[6] = bf16_lo(r.w.w); v[7] = bf16_hi(r.w.w);
-  } else {
-    float q[8];
-    if constexpr (CODE == kCodeInt8) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        q[i] = (float)(int)__builtin_amdgcn_sbfe(r.c.x, 8 * i, 8);
-        q[4 + i] = (float)(int)__builtin_amdgcn_sbfe(r.c.y, 8 * i, 8);
-      }
-    } else {
-      f32x2 d;
-      d = __builtin_amdgcn_cvt_pk_f32_fp8((int)r.c.x, false); q[0] = d.x; q[1] = d.y;
-      d = __builtin_amdgcn_cvt_pk_f32_fp8((int)r.c.x, true);  q[2] = d.x; q[3] = d.y;
-      d = __builtin_amdgcn_cvt_pk_f32_fp8((int)r.c.y, false); q[4] = d.x; q[5] = d.y;
-      d = __builtin_amdgcn_cvt_pk_f32_fp8((int)r.c.y, true);  q[6] = d.x; q[7] = d.y;
-    }
-    if constexpr (CODE == kCodeCast) {  // exact bf16 values (NaN codes stay NaN)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = q[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        const uint32_t h = pack_bf16(q[i] * r.s, q[i + 1] * r.s);  // xhat, as decompress rounds it
-        v[i] = bf16_lo(h);
-        v[i + 1] = bf16_hi(h);
-      }
-    }
-  }
+  if constexpr (!L) unpack_bf16x8(r.w, v);
+  else decode_codes8<CODE == kCodeInt8, CODE != kCodeCast>(r.c, r.s, v);
 }
 
 template <int CODE, int BLOCK, bool GL, bool UL>
@@ -101,10 +71,7 @@ __global__ __launch_bounds__(kThreads) void swiglu_bwd_kernel(const SwigluArgs a
     float g[8], u[8], d[8];
     decode_operand<CODE, GL>(rg, g);
     decode_operand<CODE, UL>(ru, u);
-    d[0] = bf16_lo(dw.x); d[1] = bf16_hi(dw.x);
-    d[2] = bf16_lo(dw.y); d[3] = bf16_hi(dw.y);
-    d[4] = bf16_lo(dw.z); d[5] = bf16_hi(dw.z);
-    d[6] = bf16_lo(dw.w); d[7] = bf16_hi(dw.w);
+    unpack_bf16x8(dw, d);
     float og[8], ou[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -115,13 +82,10 @@ __global__ __launch_bounds__(kThreads) void swiglu_bwd_kernel(const SwigluArgs a
       ou[i] = d[i] * (g[i] * sg);
       og[i] = (d[i] * u[i]) * (sg * (1.0f + g[i] * (1.0f - sg)));
     }
-    u32x4 pg, pu;
-    pg.x = pack_bf16(og[0], og[1]); pg.y = pack_bf16(og[2], og[3]);
-    pg.z = pack_bf16(og[4], og[5]); pg.w = pack_bf16(og[6], og[7]);
-    pu.x = pack_bf16(ou[0], ou[1]); pu.y = pack_bf16(ou[2], ou[3]);
-    pu.z = pack_bf16(ou[4], ou[5]); pu.w = pack_bf16(ou[6], ou[7]);
-    __builtin_nontemporal_store(pg, reinterpret_cast<u32x4 *>(a.dg + row * a.cols + col));
-    __builtin_nontemporal_store(pu, reinterpret_cast<u32x4 *>(a.du + row * a.cols + col));
+    __builtin_nontemporal_store(pack_bf16x8(og),
+                                reinterpret_cast<u32x4 *>(a.dg + row * a.cols + col));
+    __builtin_nontemporal_store(pack_bf16x8(ou),
+                                reinterpret_cast<u32x4 *>(a.du + row * a.cols + col));
   }
 }
 

@@ -54,6 +54,44 @@ class hilore_unit_desc(ctypes.Structure):
     ]
 
 
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_ELEMENT = 0, 1, 2, 3
+
+
+def _pointers(*names):
+    return [(n, ctypes.c_void_p) for n in names]
+
+
+def _int64s(*names):
+    return [(n, ctypes.c_int64) for n in names]
+
+
+class hilore_block_norm_desc(ctypes.Structure):
+    _fields_ = (_pointers("res", "y", "w_post", "gate", "w_pre", "h", "n", "codes", "code_scales",
+                          "rstd_post", "rstd_pre") + _int64s("rows", "cols", "ld_res", "ld_y")
+                + [("scale", ctypes.c_float), ("eps", ctypes.c_float),
+                   ("gate_kind", ctypes.c_int)])
+
+
+class hilore_block_norm_bwd_desc(ctypes.Structure):
+    _fields_ = ([("h", hilore_unit_desc), ("y", hilore_unit_desc)]
+                + _pointers("w_post", "gate", "w_pre", "rstd_post", "rstd_pre", "dn", "dh", "dres",
+                            "dy", "dw_post", "dw_pre", "dgate")
+                + _int64s("rows", "cols", "ld_dn")
+                + [("scale", ctypes.c_float), ("gate_kind", ctypes.c_int)])
+
+
+class hilore_int8_desc(ctypes.Structure):
+    _fields_ = (_pointers("x", "factor", "a", "a_scales", "w", "w_scales", "bias", "out")
+                + _int64s("tokens", "k", "n", "ldx", "ldo")
+                + [("out_f32", ctypes.c_int), ("accumulate", ctypes.c_int)])
+
+
+class hilore_adamw_tensor(ctypes.Structure):
+    _fields_ = (_pointers("p", "p16", "grad", "m", "v", "m_scales", "v_scales") + _int64s("n")
+                + [("lr", ctypes.c_float), ("weight_decay", ctypes.c_float),
+                   ("grad_bf16", ctypes.c_int)])
+
+
 _lib = None
 
 
@@ -98,6 +136,16 @@ def load() -> ctypes.CDLL:
         "hilore_calibrate": (i32, [i32, i32, i32, P, P, P, P, P, P, P]),
         "hilore_risk_score": (i32, [i32, P, i32, P, P, P, P, P]),
         "hilore_update_sparsity": (i32, [P, P, P, P, i32, i32, f64, P, P, P]),
+        "hilore_block_norm": (i32, [P, P]),
+        "hilore_block_norm_bwd_workspace_bytes": (ctypes.c_size_t, [P]),
+        "hilore_block_norm_bwd": (i32, [P, i32, i32, i32, P, ctypes.c_size_t, P]),
+        "hilore_int8_workspace_bytes": (ctypes.c_size_t, [P, i32]),
+        "hilore_int8_linear": (i32, [P, P, ctypes.c_size_t, P]),
+        "hilore_int8_matmul": (i32, [P, P, ctypes.c_size_t, P]),
+        "hilore_quantize_tokens": (i32, [P, P, i64, i64, i64, P, P, P]),
+        "hilore_grad_norm_workspace_bytes": (ctypes.c_size_t, [P, i32]),
+        "hilore_grad_norm": (i32, [P, i32, f64, P, P, ctypes.c_size_t, P]),
+        "hilore_adamw": (i32, [P, i32, f64, f64, f64, i64, P, ctypes.c_uint32, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -452,3 +500,251 @@ def hilore_update_sparsity(coeff, flags, adv, mask, R: int, T: int, top_frac: fl
            load().hilore_update_sparsity(_p(coeff), _p(flags), _p(adv), _p(mask), int(R), int(T),
                                          float(top_frac), _p(counts), _p(top_share),
                                          _stream(stream)))
+
+
+# ------------------------------------------------------------- layer operators --
+# Their descriptors hold the data pointers of the tensors they are made from, and a reference
+# to each (but for those of the unit descriptors given to block_norm_bwd_desc): a trainer makes
+# them once and keeps them from step to step.
+def _keeping(desc, *tensors):
+    desc._tensors = tensors
+    return desc
+
+
+def _typed(t, name: str, *dtypes: str):
+    """t, refused unless its dtype is one of `dtypes` (None passes)."""
+    if t is not None:
+        import torch
+
+        if all(t.dtype is not getattr(torch, d) for d in dtypes):
+            raise TypeError(f"{name} must be {' or '.join(dtypes)}, got {t.dtype}")
+    return t
+
+
+def _sized(t, name: str, *shape: int):
+    """t, refused unless it has that shape (None passes)."""
+    if t is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    return t
+
+
+def _rows_of(t) -> int:
+    """Elements between the rows of a 2-D tensor (a single row's stride says nothing)."""
+    if t is None:
+        return 0
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0)) // 8 * 8
+
+
+def _gate_kind(gate, rows: int, cols: int) -> int:
+    """A gate's kind from its shape: [cols], [rows, 1] or [rows, cols]."""
+    if gate is None:
+        return GATE_NONE
+    kinds = {(cols,): GATE_CHANNEL, (rows, 1): GATE_TOKEN, (rows, cols): GATE_ELEMENT}
+    if tuple(gate.shape) not in kinds:
+        raise ValueError(f"gate must be [{cols}], [{rows}, 1] or [{rows}, {cols}], got "
+                         f"{tuple(gate.shape)}")
+    return kinds[tuple(gate.shape)]
+
+
+def block_norm_desc(res, y=None, w_post=None, gate=None, scale: float = 1.0, w_pre=None,
+                    eps: float = 1e-6, h=None, n=None, codes=None, code_scales=None,
+                    rstd_post=None, rstd_pre=None) -> hilore_block_norm_desc:
+    """Descriptor of hilore_block_norm: res and y bf16 [rows, cols] (rows may be padded),
+    weights bf16 [cols], gate bf16 [cols], [rows, 1] or [rows, cols]; outputs h and n
+    bf16, codes int8 with code_scales f32 [rows], rstd_* f32 [rows]."""
+    rows, cols = (int(d) for d in res.shape)
+    for t, name in ((res, "res"), (y, "y"), (h, "h"), (n, "n")):
+        _sized(_typed(t, name, "bfloat16"), name, rows, cols)
+    for t, name in ((w_post, "w_post"), (w_pre, "w_pre")):
+        _sized(_typed(t, name, "bfloat16"), name, cols)
+    for t, name in ((code_scales, "code_scales"), (rstd_post, "rstd_post"), (rstd_pre, "rstd_pre")):
+        _sized(_typed(t, name, "float32"), name, rows)
+    _sized(_typed(codes, "codes", "int8"), "codes", rows, cols)
+    _typed(gate, "gate", "bfloat16")
+    desc = hilore_block_norm_desc(_p_rows(res), _p_rows(y), _p(w_post), _p(gate), _p(w_pre), _p(h),
+                                  _p(n), _p(codes), _p(code_scales), _p(rstd_post), _p(rstd_pre),
+                                  rows, cols, _rows_of(res), _rows_of(y), float(scale), float(eps),
+                                  _gate_kind(gate, rows, cols))
+    return _keeping(desc, res, y, w_post, gate, w_pre, h, n, codes, code_scales, rstd_post,
+                    rstd_pre)
+
+
+def hilore_block_norm(desc: hilore_block_norm_desc, stream=None):
+    """h = res + scale * gate * norm(y) * w_post and n = norm(h) * w_pre, in one pass."""
+    _check("hilore_block_norm", load().hilore_block_norm(ctypes.byref(desc), _stream(stream)))
+
+
+def block_norm_bwd_desc(h=None, y=None, w_post=None, gate=None, scale: float = 1.0, w_pre=None,
+                        rstd_post=None, rstd_pre=None, dn=None, dh=None, dres=None, dy=None,
+                        dw_post=None, dw_pre=None, dgate=None) -> hilore_block_norm_bwd_desc:
+    """Descriptor of hilore_block_norm_bwd: h and y unit descriptors (codes for an L unit,
+    else bf16 x), dn (rows may be padded), dh, dres and dy bf16 [rows, cols], dw_* f32 [cols],
+    dgate f32 [cols] or [rows, 1], or bf16 [rows, cols], like the gate."""
+    ref = dn if dn is not None else dh
+    rows, cols = (int(d) for d in ref.shape)
+    for t, name in ((dn, "dn"), (dh, "dh"), (dres, "dres"), (dy, "dy")):
+        _sized(_typed(t, name, "bfloat16"), name, rows, cols)
+    for t, name in ((w_post, "w_post"), (w_pre, "w_pre")):
+        _sized(_typed(t, name, "bfloat16"), name, cols)
+    for t, name in ((dw_post, "dw_post"), (dw_pre, "dw_pre")):
+        _sized(_typed(t, name, "float32"), name, cols)
+    for t, name in ((rstd_post, "rstd_post"), (rstd_pre, "rstd_pre")):
+        _sized(_typed(t, name, "float32"), name, rows)
+    kind = _gate_kind(_typed(gate, "gate", "bfloat16"), rows, cols)
+    if dgate is not None:
+        if gate is None:
+            raise ValueError("dgate without a gate")
+        _sized(_typed(dgate, "dgate", "bfloat16" if kind == GATE_ELEMENT else "float32"), "dgate",
+               *gate.shape)
+    none = hilore_unit_desc()
+    desc = hilore_block_norm_bwd_desc(none if h is None else h, none if y is None else y, _p(w_post),
+                                      _p(gate), _p(w_pre), _p(rstd_post), _p(rstd_pre), _p_rows(dn),
+                                      _p(dh), _p(dres), _p(dy), _p(dw_post), _p(dw_pre), _p(dgate),
+                                      rows, cols, _rows_of(dn), float(scale), kind)
+    return _keeping(desc, w_post, gate, w_pre, rstd_post, rstd_pre, dn, dh, dres, dy, dw_post,
+                    dw_pre, dgate)
+
+
+def hilore_block_norm_bwd_workspace_bytes(desc: hilore_block_norm_bwd_desc) -> int:
+    return int(load().hilore_block_norm_bwd_workspace_bytes(ctypes.byref(desc)))
+
+
+def hilore_block_norm_bwd(desc: hilore_block_norm_bwd_desc, code=0, block: int = 0,
+                          accumulate: bool = False, workspace=None, stream=None):
+    """Gradients of hilore_block_norm.  code and block are those of the L units among h and y
+    (not read without one).  workspace: a device tensor of at least
+    hilore_block_norm_bwd_workspace_bytes(desc) bytes, or None (taken from torch's allocator)."""
+    need = hilore_block_norm_bwd_workspace_bytes(desc) if workspace is None else 0
+    wp, wb, _keep = _workspace(workspace, need, stream)
+    _check("hilore_block_norm_bwd",
+           load().hilore_block_norm_bwd(ctypes.byref(desc), _code(code), int(block),
+                                        1 if accumulate else 0, wp, wb, _stream(stream)))
+
+
+def int8_desc(w, out, x=None, factor=None, a=None, a_scales=None, w_scales=None, bias=None,
+              accumulate: bool = False) -> hilore_int8_desc:
+    """Descriptor of an int8 product: w int8 [n, k] with w_scales f32 [n]; out bf16 or f32
+    [tokens, n]; x bf16 [tokens, k] with an optional factor f32 [k] (hilore_int8_linear), or a
+    int8 [tokens, k] with a_scales f32 [tokens] (hilore_int8_matmul); rows of x and out may be
+    padded."""
+    n, k = (int(d) for d in w.shape)
+    tokens = int(out.shape[0])
+    _typed(w, "w", "int8")
+    _sized(_typed(out, "out", "bfloat16", "float32"), "out", tokens, n)
+    _sized(_typed(x, "x", "bfloat16"), "x", tokens, k)
+    _sized(_typed(factor, "factor", "float32"), "factor", k)
+    _sized(_typed(a, "a", "int8"), "a", tokens, k)
+    _sized(_typed(a_scales, "a_scales", "float32"), "a_scales", tokens)
+    _sized(_typed(w_scales, "w_scales", "float32"), "w_scales", n)
+    _sized(_typed(bias, "bias", "bfloat16"), "bias", n)
+    if x is None and a is None:
+        raise ValueError("a product needs x or a")
+    desc = hilore_int8_desc(_p_rows(x), _p(factor), _p(a), _p(a_scales), _p(w), _p(w_scales),
+                            _p(bias), _p_rows(out), tokens, k, n, _rows_of(x), _rows_of(out),
+                            0 if out.element_size() == 2 else 1, 1 if accumulate else 0)
+    return _keeping(desc, x, factor, a, a_scales, w, w_scales, bias, out)
+
+
+def hilore_int8_workspace_bytes(desc: hilore_int8_desc, quantize: Optional[bool] = None) -> int:
+    """quantize: of hilore_int8_linear (True) or hilore_int8_matmul; None: by whether the
+    descriptor has an x."""
+    q = bool(desc.x) if quantize is None else quantize
+    return int(load().hilore_int8_workspace_bytes(ctypes.byref(desc), 1 if q else 0))
+
+
+def _int8(fn: str, desc, quantize: bool, workspace, stream):
+    need = hilore_int8_workspace_bytes(desc, quantize) if workspace is None else 0
+    wp, wb, _keep = _workspace(workspace, need, stream)
+    _check(fn, getattr(load(), fn)(ctypes.byref(desc), wp, wb, _stream(stream)))
+
+
+def hilore_int8_linear(desc: hilore_int8_desc, workspace=None, stream=None):
+    """out (+)= round8(x * factor) w^T, scaled, with bias.  workspace: a device tensor of at
+    least hilore_int8_workspace_bytes(desc) bytes, or None (taken from torch's allocator)."""
+    _int8("hilore_int8_linear", desc, True, workspace, stream)
+
+
+def hilore_int8_matmul(desc: hilore_int8_desc, workspace=None, stream=None):
+    """out (+)= a w^T, scaled, with bias; workspace as for hilore_int8_linear."""
+    _int8("hilore_int8_matmul", desc, False, workspace, stream)
+
+
+def hilore_quantize_tokens(x, codes, scales, factor=None, stream=None):
+    """codes int8 [tokens, k] and scales f32 [tokens] of x * factor, row by row."""
+    tokens, k = (int(d) for d in x.shape)
+    _typed(x, "x", "bfloat16")
+    _sized(_typed(codes, "codes", "int8"), "codes", tokens, k)
+    _sized(_typed(scales, "scales", "float32"), "scales", tokens)
+    _sized(_typed(factor, "factor", "float32"), "factor", k)
+    _check("hilore_quantize_tokens",
+           load().hilore_quantize_tokens(_p_rows(x), _p(factor), tokens, k, _rows_of(x), _p(codes),
+                                         _p(scales), _stream(stream)))
+
+
+ADAMW_BLOCK = 256  # elements per scale of an 8-bit state
+
+
+def adamw_tensor(grad, m, v, p=None, p16=None, m_scales=None, v_scales=None, lr: float = 1e-3,
+                 weight_decay: float = 0.0) -> hilore_adamw_tensor:
+    """Descriptor of one tensor of an optimizer step (any shape, dense): p f32 and / or p16
+    bf16, grad f32 or bf16, states m and v f32, or E4M3FN codes (float8_e4m3fn or uint8) with
+    m_scales and v_scales f32 [ceil(n / 256)]."""
+    n = int(grad.numel())
+    eight = m_scales is not None or v_scales is not None
+    state = ("float8_e4m3fn", "uint8") if eight else ("float32",)
+    _typed(p, "p", "float32"), _typed(p16, "p16", "bfloat16")
+    _typed(grad, "grad", "float32", "bfloat16")
+    _typed(m, "m", *state), _typed(v, "v", *state)
+    _typed(m_scales, "m_scales", "float32"), _typed(v_scales, "v_scales", "float32")
+    for t, name in ((p, "p"), (p16, "p16"), (m, "m"), (v, "v")):
+        if t is not None and t.numel() != n:
+            raise ValueError(f"{name} has {t.numel()} elements, the gradient {n}")
+    for t, name in ((m_scales, "m_scales"), (v_scales, "v_scales")):
+        if t is not None and t.numel() != -(-n // ADAMW_BLOCK):
+            raise ValueError(f"{name} needs {-(-n // ADAMW_BLOCK)} elements, got {t.numel()}")
+    desc = hilore_adamw_tensor(_p(p), _p(p16), _p(grad), _p(m), _p(v), _p(m_scales), _p(v_scales), n,
+                               float(lr), float(weight_decay), 1 if grad.element_size() == 2 else 0)
+    return _keeping(desc, p, p16, grad, m, v, m_scales, v_scales)
+
+
+def adamw_tensors(tensors: Sequence[hilore_adamw_tensor]):
+    """The descriptors as one array, which a trainer keeps from step to step (a learning rate
+    changes by array[i].lr = ...)."""
+    return _keeping((hilore_adamw_tensor * len(tensors))(*tensors), *tensors)
+
+
+def _tensor_array(tensors):
+    return tensors if isinstance(tensors, ctypes.Array) else adamw_tensors(tensors)
+
+
+def hilore_grad_norm_workspace_bytes(tensors) -> int:
+    arr = _tensor_array(tensors)
+    return int(load().hilore_grad_norm_workspace_bytes(arr, len(arr)))
+
+
+def hilore_grad_norm(tensors, max_norm: float, norm, workspace=None, stream=None):
+    """norm (f32 device tensor of 2) = the gradients' global norm and the factor that clips it to
+    max_norm.  workspace: a device tensor of at least hilore_grad_norm_workspace_bytes(tensors)
+    bytes, or None (taken from torch's allocator)."""
+    arr = _tensor_array(tensors)
+    if norm.numel() != 2:
+        raise ValueError(f"norm must have 2 elements, got {norm.numel()}")
+    _typed(norm, "norm", "float32")
+    need = hilore_grad_norm_workspace_bytes(arr) if workspace is None else 0
+    wp, wb, _keep = _workspace(workspace, need, stream)
+    _check("hilore_grad_norm",
+           load().hilore_grad_norm(arr, len(arr), float(max_norm), _p(norm), wp, wb,
+                                   _stream(stream)))
+
+
+def hilore_adamw(tensors, beta1: float, beta2: float, eps: float, step: int, norm=None,
+                 seed: int = 0, stream=None):
+    """One AdamW step over all tensors (a sequence of adamw_tensor or an array of
+    adamw_tensors); norm as hilore_grad_norm writes it, or None for no clipping."""
+    arr = _tensor_array(tensors)
+    if norm is not None and norm.numel() != 2:
+        raise ValueError(f"norm must have 2 elements, got {norm.numel()}")
+    _check("hilore_adamw",
+           load().hilore_adamw(arr, len(arr), float(beta1), float(beta2), float(eps), int(step),
+                               _p(_typed(norm, "norm", "float32")), int(seed) & 0xFFFFFFFF,
+                               _stream(stream)))
