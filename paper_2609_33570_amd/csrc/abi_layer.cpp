@@ -128,10 +128,11 @@ hilore_status check_int8(const hilore_int8_desc &d, bool quantize) {
   if (d.tokens == 0 || d.n == 0) return HILORE_OK;
   if (!d.out || d.ldo < d.n) return HILORE_ERR_INVALID_ARG;
   if (d.ldo % 8 != 0) return HILORE_ERR_ALIGNMENT;
+  if (!quantize && !d.a_scales) return HILORE_ERR_INVALID_ARG;
   if (d.k > 0) {
     if (!d.w) return HILORE_ERR_INVALID_ARG;
     if (quantize && (!d.x || d.ldx < d.k)) return HILORE_ERR_INVALID_ARG;
-    if (!quantize && (!d.a || !d.a_scales)) return HILORE_ERR_INVALID_ARG;
+    if (!quantize && !d.a) return HILORE_ERR_INVALID_ARG;
     if (quantize && d.ldx % 8 != 0) return HILORE_ERR_ALIGNMENT;
   }
   const void *ptrs[] = {quantize ? d.x : nullptr, quantize ? d.factor : nullptr,
