@@ -16,84 +16,289 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------- rounding of tokens --
-constexpr int kQuantThreads = 256;
+constexpr int kQuantThreads = 1024;  // at most
+constexpr int64_t kQuantHeld = 4 * 8 * kQuantThreads;  // longest row held in registers
 
 // 8 values of x * factor at col.
 __device__ __forceinline__ void load_scaled8(const uint16_t *x, const float *factor, int64_t col,
                                              float v[8]) {
   unpack_bf16x8(*reinterpret_cast<const u32x4 *>(x + col), v);
   if (factor) {
+    const f32x4 lo = *reinterpret_cast<const f32x4 *>(factor + col);
+    const f32x4 hi = *reinterpret_cast<const f32x4 *>(factor + col + 4);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= factor[col + i];
+    for (int i = 0; i < 4; ++i) {
+      v[i] *= lo[i];
+      v[4 + i] *= hi[i];
+    }
   }
 }
 
+// A workgroup rounds a row at a time: its largest magnitude, then its codes.  Bound by HBM (3 B
+// an element) for many tokens, by latency for few.  V > 0: the row stays in registers in
+// between, V pieces of 8 values a thread; V = 0: longer rows are read twice.
+template <int V>
 __global__ __launch_bounds__(kQuantThreads) void quantize_kernel(const QuantArgs a) {
-  __shared__ uint32_t lds[kQuantThreads / kWave];
-  for (int64_t row = blockIdx.x; row < a.tokens; row += gridDim.x) {
-  const uint16_t *x = a.x + row * a.ldx;
-  uint32_t top = 0;
-  for (int64_t col = threadIdx.x * 8; col < a.k; col += kQuantThreads * 8) {
-    float v[8];
-    load_scaled8(x, a.factor, col, v);
+  __shared__ uint32_t lds[2][kQuantThreads / kWave];
+  const int waves = blockDim.x / kWave;
+  const int64_t stride = (int64_t)blockDim.x * 8, first = (int64_t)threadIdx.x * 8;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.tokens; row += gridDim.x, turn ^= 1) {
+    const uint16_t *x = a.x + row * a.ldx;
+    float v[V > 0 ? V : 1][8];
+    uint32_t top = 0;
+    if constexpr (V > 0) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(fabsf(v[i])));
-  }
-  top = group_max_u32<32>(top);
-  top = max(top, (uint32_t)__shfl_xor((int)top, 32, kWave));
-  __syncthreads();  // of the row before
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
-  __syncthreads();
-  for (int w = 0; w < kQuantThreads / kWave; ++w) top = max(top, lds[w]);
-  float scale;
-  const float r = token_scale(__uint_as_float(top), scale);
-  if (threadIdx.x == 0) a.scales[row] = scale;
-  for (int64_t col = threadIdx.x * 8; col < a.k; col += kQuantThreads * 8) {
-    float v[8];
-    load_scaled8(x, a.factor, col, v);
-    *reinterpret_cast<u32x2 *>(a.codes + row * a.k + col) = token_codes8(v, r);
-  }
+      for (int j = 0; j < V; ++j)
+        if (first + j * stride < a.k) {
+          load_scaled8(x, a.factor, first + j * stride, v[j]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
+        }
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(fabsf(v[j][i])));
+    } else {
+      for (int64_t col = first; col < a.k; col += stride) {
+        load_scaled8(x, a.factor, col, v[0]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(fabsf(v[0][i])));
+      }
+    }
+    top = group_max_u32<32>(top);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32, kWave));
+    if ((threadIdx.x & 63) == 0) lds[turn][threadIdx.x >> 6] = top;
+    __syncthreads();
+    for (int w = 0; w < waves; ++w) top = max(top, lds[turn][w]);
+    float scale;
+    const float r = token_scale(__uint_as_float(top), scale);
+    if (threadIdx.x == 0) a.scales[row] = scale;
+    int8_t *codes = a.codes + row * a.k;
+    if constexpr (V > 0) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (first + j * stride < a.k)
+          *reinterpret_cast<u32x2 *>(codes + first + j * stride) = token_codes8(v[j], r);
+    } else {
+      for (int64_t col = first; col < a.k; col += stride) {
+        load_scaled8(x, a.factor, col, v[0]);
+        *reinterpret_cast<u32x2 *>(codes + col) = token_codes8(v[0], r);
+      }
+    }
   }
 }
 
 // ------------------------------------------------------------------ product --
-// One value of the output: the exact sum, scaled, with bias, added or written.
-__device__ __forceinline__ void finish(const Int8Args &a, int64_t t, int64_t n, int sum) {
-  float v = (float)sum * a.a_scales[t];
-  if (a.w_scales) v *= a.w_scales[n];
-  if (a.bias) v += __uint_as_float((uint32_t)a.bias[n] << 16);
+// Four neighbouring values of the output (n % 4 == 0): the exact sums, scaled, with bias,
+// added or written.
+__device__ __forceinline__ void finish4(const Int8Args &a, int64_t t, int64_t n, i32x4 sum) {
+  const float sa = a.a_scales[t];
+  f32x4 v = {(float)sum.x * sa, (float)sum.y * sa, (float)sum.z * sa, (float)sum.w * sa};
+  if (a.w_scales) v *= *reinterpret_cast<const f32x4 *>(a.w_scales + n);
+  if (a.bias) {
+    const u32x2 b = *reinterpret_cast<const u32x2 *>(a.bias + n);
+    v += f32x4{bf16_lo(b.x), bf16_hi(b.x), bf16_lo(b.y), bf16_hi(b.y)};
+  }
   if (a.out_f32) {
-    float *o = static_cast<float *>(a.out) + t * a.ldo + n;
+    f32x4 *o = reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + t * a.ldo + n);
     *o = a.accumulate ? *o + v : v;
   } else {
-    uint16_t *o = static_cast<uint16_t *>(a.out) + t * a.ldo + n;
-    if (a.accumulate) v += __uint_as_float((uint32_t)*o << 16);
-    *o = (uint16_t)pack_bf16(v, 0.0f);
+    u32x2 *o = reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.out) + t * a.ldo + n);
+    if (a.accumulate) {
+      const u32x2 p = *o;
+      v += f32x4{bf16_lo(p.x), bf16_hi(p.x), bf16_lo(p.y), bf16_hi(p.y)};
+    }
+    *o = u32x2{pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)};
   }
 }
 
-// 64 x 64 outputs per workgroup, 32 x 32 per wave, operands straight from memory.
-__global__ __launch_bounds__(256) void int8_kernel(const Int8Args a) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const uint32_t tiles_n = (uint32_t)((a.n + 63) / 64);
-  const int64_t t0 = (int64_t)(blockIdx.x / tiles_n) * 64 + (wave >> 1) * 32;
-  const int64_t n0 = (int64_t)(blockIdx.x % tiles_n) * 64 + (wave & 1) * 32;
-  const int64_t ta = t0 + (lane & 31) < a.tokens ? t0 + (lane & 31) : a.tokens - 1;
-  const int64_t nb = n0 + (lane & 31) < a.n ? n0 + (lane & 31) : a.n - 1;
-  const int8_t *pa = a.a + ta * a.k, *pb = a.w + nb * a.k;
-  i32x16 acc = {};
-  for (int k = (lane >> 5) * 16; k < a.k + (lane >> 5) * 16; k += 32) {
-    i32x4 x = {}, y = {};
-    if (k < a.k) {
-      x = *reinterpret_cast<const i32x4 *>(pa + k);
-      y = *reinterpret_cast<const i32x4 *>(pb + k);
-    }
-    acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, y, acc, 0, 0, 0);
-  }
+constexpr uint32_t kOob = 0x80000000u;  // a buffer offset past every range: loads 0
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// The workgroup's barrier after this wave's LDS reads and all but its N newest vector-memory
+// operations.  (__syncthreads would wait for every LDS-DMA load in flight.)
+template <int N>
+__device__ __forceinline__ void barrier_but_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt is 6 bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));  // lgkmcnt 0
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// --------------------------------------------------------------- few tokens --
+// Up to 64 tokens: the product streams the weights once.  A workgroup owns 16 NB channels
+// and a range of k (a part); its waves take k-steps of 64 G bytes in turn and add their sums
+// in LDS.  Both operands pass through the wave's own LDS by LDS-DMA, 64 G bytes of a row by 4 G
+// neighbouring lanes: straight into v_mfma_i32_16x16x64_i8's registers every lane would
+// read another row, and the address unit, which takes a cycle for each 128-byte line, not
+// the memory, would set the pace (64 x 18944 x 3584: 27.8 us).  Four slots, three in
+// flight; no barriers.  Several parts leave their sums in the workspace for int8_join_kernel.
+constexpr int kSlots = 4;
+
+// Rows of one slot: 16 NB channels, then 16 TB tokens, 64 G bytes each; 16-byte chunk c of row
+// r lies at c ^ swz(r), so that a fragment read's 8 lanes of a cycle, on 8 rows, meet all banks.
+template <int G>
+__device__ __forceinline__ int few_swz(int row) {
+  static_assert(G == 1 || G == 2, "bytes of a row in a slot");
+  return G == 1 ? (row >> 1) & 3 : row & 7;
+}
+
+template <int TB, int NB, int G>
+struct FewLoad {
+  static constexpr int kRows = 16 / G;  // rows of one load
+  static constexpr int kLoads = (TB + NB) * G;
+  static constexpr int kSlotBytes = kLoads * 1024;
+  uint32_t first;  // the lane's row of load 0, times k
+  uint32_t step;   // kRows k
+  int chunk;       // the lane's first byte within a slot's k
+};
+
+template <int TB, int NB, int G>
+__device__ __forceinline__ void dma_few(const FewLoad<TB, NB, G> &f, __amdgpu_buffer_rsrc_t rw,
+                                        __amdgpu_buffer_rsrc_t rx, int k, int end, uint8_t *slot) {
+  const int kk = k + f.chunk;
+  const uint32_t off = kk < end ? f.first + (uint32_t)kk : kOob;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int64_t t = t0 + (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3), n = n0 + (lane & 31);
-    if (t < a.tokens && n < a.n) finish(a, t, n, acc[r]);
+  for (int j = 0; j < NB * G; ++j)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void *)(slot + j * 1024), 16,
+                                             (int)(off + j * f.step), 0, 0, 0);
+#pragma unroll
+  for (int j = 0; j < TB * G; ++j)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void *)(slot + (NB * G + j) * 1024), 16,
+                                             (int)(off + j * f.step), 0, 0, 0);
+}
+
+// The products of one slot; `at`: the lane's fragment offset of each k-step of 64.
+template <int TB, int NB, int G>
+__device__ __forceinline__ void mma_few(i32x4 (&acc)[NB][TB], const uint8_t *slot,
+                                        const uint32_t (&at)[G]) {
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    i32x4 w[NB], x[TB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+      w[i] = *reinterpret_cast<const i32x4 *>(slot + at[g] + i * (16 * 64 * G));
+#pragma unroll
+    for (int j = 0; j < TB; ++j)
+      x[j] = *reinterpret_cast<const i32x4 *>(slot + at[g] + (NB + j) * (16 * 64 * G));
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < TB; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], x[j], acc[i][j], 0, 0, 0);
+  }
+}
+
+// One slot's turn: the loads of the slot three turns ahead, then the wait for this one's.
+template <int TB, int NB, int G>
+__device__ __forceinline__ void few_turn(i32x4 (&acc)[NB][TB], const FewLoad<TB, NB, G> &f,
+                                         __amdgpu_buffer_rsrc_t rw, __amdgpu_buffer_rsrc_t rx,
+                                         int k_ahead, int end, const uint8_t *cur, uint8_t *ahead,
+                                         const uint32_t (&at)[G]) {
+  constexpr int N = (kSlots - 1) * FewLoad<TB, NB, G>::kLoads;
+  static_assert(N < 64, "vmcnt is 6 bits");
+  // the reads of `ahead`'s last turn have been waited for by its products
+  dma_few(f, rw, rx, k_ahead, end, ahead);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  mma_few<TB, NB, G>(acc, cur, at);
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int TB, int NB, int G, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void int8_few_kernel(const Int8Args a, int parts) {
+  using Load = FewLoad<TB, NB, G>;
+  constexpr int kSlot = Load::kSlotBytes;
+  __shared__ __attribute__((aligned(16))) uint8_t s0[WAVES * kSlot], s1[WAVES * kSlot];
+  __shared__ __attribute__((aligned(16))) uint8_t s2[WAVES * kSlot], s3[WAVES * kSlot];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int tile = blockIdx.x / parts, part = blockIdx.x - tile * parts;
+  const int64_t n0 = (int64_t)__builtin_amdgcn_readfirstlane(tile) * (16 * NB);
+  const int64_t rows = a.n - n0 < 16 * NB ? a.n - n0 : 16 * NB;
+  const __amdgpu_buffer_rsrc_t rw =
+      __builtin_amdgcn_make_buffer_rsrc((void *)(a.w + n0 * a.k), 0, (int)(rows * a.k), 0x00020000);
+  const __amdgpu_buffer_rsrc_t rx =
+      __builtin_amdgcn_make_buffer_rsrc((void *)a.a, 0, (int)(a.tokens * a.k), 0x00020000);
+  // this part's k-steps of 64 G
+  const int steps = (a.k + 64 * G - 1) / (64 * G);  // <= 2^11, of at most 2^9 parts
+  const int g0 = (int)((unsigned)(steps * part) / (unsigned)parts);
+  const int g1 = (int)((unsigned)(steps * (part + 1)) / (unsigned)parts);
+  const int end = g1 * 64 * G < a.k ? g1 * 64 * G : a.k;
+
+  Load f;
+  {
+    const int row = lane / (4 * G);
+    f.first = (uint32_t)row * (uint32_t)a.k;
+    f.step = (uint32_t)Load::kRows * (uint32_t)a.k;
+    f.chunk = ((lane & (4 * G - 1)) ^ few_swz<G>(row)) * 16;  // kRows % 8 == 0: the same in all loads
+  }
+  uint32_t at[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int r = lane & 15, c = g * 4 + (lane >> 4);
+    at[g] = (uint32_t)(r * 64 * G + ((c ^ few_swz<G>(r)) << 4));
+  }
+  i32x4 acc[NB][TB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int j = 0; j < TB; ++j) acc[i][j] = i32x4{};
+
+  uint8_t *const p0 = s0 + wave * kSlot, *const p1 = s1 + wave * kSlot;
+  uint8_t *const p2 = s2 + wave * kSlot, *const p3 = s3 + wave * kSlot;
+  constexpr int kTurn = WAVES * 64 * G;
+  int k = (g0 + wave) * 64 * G;
+  dma_few(f, rw, rx, k, end, p0);
+  dma_few(f, rw, rx, k + kTurn, end, p1);
+  dma_few(f, rw, rx, k + 2 * kTurn, end, p2);
+  for (; k < end; k += 4 * kTurn) {  // loads past the end read nothing and give zeros
+    few_turn(acc, f, rw, rx, k + 3 * kTurn, end, p0, p3, at);
+    few_turn(acc, f, rw, rx, k + 4 * kTurn, end, p1, p0, at);
+    few_turn(acc, f, rw, rx, k + 5 * kTurn, end, p2, p1, at);
+    few_turn(acc, f, rw, rx, k + 6 * kTurn, end, p3, p2, at);
+  }
+  // sums of the waves: 1 KB per accumulator block, in the wave's place of s0, then of s1
+  barrier_but_vmcnt<0>();
+  constexpr int kPerSlot = kSlot / 1024;
+  static_assert(NB * TB <= 2 * kPerSlot, "sums fit two slots");
+  const auto place = [&](int w, int b) {
+    uint8_t *p = b < kPerSlot ? s0 + w * kSlot + b * 1024 : s1 + w * kSlot + (b - kPerSlot) * 1024;
+    return reinterpret_cast<i32x4 *>(p) + lane;
+  };
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int j = 0; j < TB; ++j) *place(wave, i * TB + j) = acc[i][j];
+  __syncthreads();
+  // accumulator block (i, j): lane l holds token l % 16 of block j, channels 4 (l / 16) .. of i
+  for (int b = wave; b < NB * TB; b += WAVES) {
+    i32x4 sum = *place(0, b);
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum += *place(w, b);
+    const int64_t t = (b % TB) * 16 + (lane & 15), n = n0 + (b / TB) * 16 + (lane >> 4) * 4;
+    if (t >= a.tokens || n >= a.n) continue;
+    if (parts == 1) finish4(a, t, n, sum);
+    else *reinterpret_cast<i32x4 *>(a.part + ((int64_t)part * a.tokens + t) * a.n + n) = sum;
+  }
+}
+
+// The sums of `parts` partial products ([part][token][channel] in the workspace).
+__global__ __launch_bounds__(256) void int8_join_kernel(const Int8Args a, int parts) {
+  const uint32_t quads = (uint32_t)a.n / 4, all = (uint32_t)a.tokens * quads;  // < 64 * 2^24
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) {
+    const i32x4 *p = reinterpret_cast<const i32x4 *>(a.part) + i;
+    i32x4 sum = *p;
+#pragma unroll 8
+    for (int s = 1; s < parts; ++s) sum += p[(int64_t)s * all];
+    const uint32_t t = i / quads;
+    finish4(a, t, (int64_t)(i - t * quads) * 4, sum);
   }
 }
 
@@ -108,9 +313,6 @@ constexpr int kTile = 256, kStageK = 64, kTileThreads = 256;
 constexpr int kStageBytes = kTile * kStageK;  // of one operand (16 KB)
 constexpr int kStageLoads = 8;                // LDS-DMA instructions of a wave per stage
 constexpr int kGroupT = 8;
-constexpr uint32_t kOob = 0x80000000u;        // a buffer offset past every range: loads 0
-
-typedef __attribute__((address_space(3))) void lds_void;
 
 struct TileLoad {
   uint32_t a[4], b[4];  // byte offset of the lane's chunk in its row of each load, at k = 0
@@ -130,18 +332,6 @@ __device__ __forceinline__ void dma_stage(__amdgpu_buffer_rsrc_t ra, __amdgpu_bu
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void *)(lb + (wave * 64 + r * 16) * kStageK),
                                              16, (int)((tl.b[r] + (uint32_t)k0) | past), 0, 0, 0);
   }
-}
-
-// The workgroup's barrier after this wave's LDS reads and all but its N newest vector-memory
-// operations.  (__syncthreads would wait for every LDS-DMA load in flight.)
-template <int N>
-__device__ __forceinline__ void barrier_but_vmcnt() {
-  static_assert(N >= 0 && N < 64, "vmcnt is 6 bits");
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));  // lgkmcnt 0
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
 }
 
 struct TileFrags {
@@ -385,25 +575,82 @@ __global__ __launch_bounds__(kTileThreads, 1) void int8_tile_kernel(const Int8Ar
 
 hipError_t launch_quantize_tokens(const QuantArgs &a, hipStream_t s) {
   if (a.tokens == 0) return hipSuccess;
-  const unsigned groups = (unsigned)(a.tokens < (1 << 20) ? a.tokens : 1 << 20);
-  hipLaunchKernelGGL(quantize_kernel, dim3(groups), dim3(kQuantThreads), 0, s, a);
+  // few tokens: as many threads as there are pieces; many: two pieces a thread (16384 x 3584
+  // with 1 / 2 / 4: 42.5 / 34.5 / 37.4 us, x 8192 with 2 / 4: 68.8 / 75.3; 5.1 to 5.9 TB/s)
+  const int64_t pieces = (a.k + 7) / 8;
+  const int v = a.k > kQuantHeld ? 0
+                : a.tokens < 1024 ? (pieces <= 1024 ? 1 : pieces <= 2048 ? 2 : 4)
+                                  : (pieces <= 256 ? 1 : pieces <= 1024 ? 2 : 4);
+  int64_t threads = v == 0 ? kQuantThreads : ((pieces + v - 1) / v + kWave - 1) / kWave * kWave;
+  if (threads < kWave) threads = kWave;
+  const dim3 grid((unsigned)(a.tokens < (1 << 20) ? a.tokens : 1 << 20)), block((unsigned)threads);
+  if (v == 1) hipLaunchKernelGGL(quantize_kernel<1>, grid, block, 0, s, a);
+  else if (v == 2) hipLaunchKernelGGL(quantize_kernel<2>, grid, block, 0, s, a);
+  else if (v == 4) hipLaunchKernelGGL(quantize_kernel<4>, grid, block, 0, s, a);
+  else hipLaunchKernelGGL(quantize_kernel<0>, grid, block, 0, s, a);
   return hipGetLastError();
 }
 
-size_t int8_part_bytes(int64_t, int64_t, int64_t) { return 0; }
+namespace {
+
+// How a product of up to kFewTokens tokens runs.  A workgroup of 128 KB of LDS has a CU to
+// itself and waits 2 to 3 us for its first operands, so what counts is that the workgroups
+// fill the chip once: k is split into as many parts as whole blocks of channels fit 256
+// CUs (18944 x 3584: 16 tokens, 1 / 2 parts 16.5 / 21.9 us; 64 tokens, 4 / 9 parts 25.6 / 28.4),
+// but a part keeps 2048 k for the price of the second launch (4.5 us).  Up to 16 tokens the
+// 16-channel blocks of more than 256 CUs' worth go as 32-channel workgroups of 48 KB
+// instead, three to a CU (1 x 3584 x 4608 7.6 -> 5.1 us, x 18944 21.6 -> 15.5).
+constexpr int kFewTokens = 64;
+struct FewPlan {
+  int channels, parts;  // channels of a workgroup
+};
+
+FewPlan few_plan(int64_t tokens, int64_t k, int64_t n) {
+  FewPlan p{};
+  p.channels = tokens > 32 ? 64 : tokens > 16 || n > 16 * 256 ? 32 : 16;
+  const int64_t tiles = (n + p.channels - 1) / p.channels;
+  int64_t parts = 256 / tiles;
+  if (parts > k / 2048) parts = k / 2048;
+  p.parts = parts < 1 ? 1 : (int)parts;
+  return p;
+}
+
+template <int TB, int NB, int G, int WAVES>
+void launch_few(const Int8Args &a, const FewPlan &p, hipStream_t s) {
+  const int64_t tiles = (a.n + 16 * NB - 1) / (16 * NB);
+  hipLaunchKernelGGL((int8_few_kernel<TB, NB, G, WAVES>), dim3((unsigned)(tiles * p.parts)),
+                     dim3(WAVES * 64), 0, s, a, p.parts);
+  if (p.parts > 1) {
+    const int64_t groups = (a.tokens * (a.n / 4) + 255) / 256;
+    hipLaunchKernelGGL(int8_join_kernel, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0,
+                       s, a, p.parts);
+  }
+}
+
+}  // namespace
+
+size_t int8_part_bytes(int64_t tokens, int64_t k, int64_t n) {
+  if (tokens > kFewTokens || tokens <= 0 || n <= 0) return 0;
+  const FewPlan p = few_plan(tokens, k, n);
+  return p.parts > 1 ? (size_t)p.parts * (size_t)tokens * (size_t)n * sizeof(int32_t) : 0;
+}
 
 hipError_t launch_int8(const Int8Args &a, hipStream_t s) {
   if (a.tokens == 0 || a.n == 0) return hipSuccess;
-  if (a.tokens > 64) {
-    const int tiles_t = (int)((a.tokens + kTile - 1) / kTile), tiles_n = (int)((a.n + kTile - 1) / kTile);
-    if (a.out_f32 || a.accumulate)
-      hipLaunchKernelGGL(int8_tile_kernel<true>, dim3(tiles_t * tiles_n), dim3(kTileThreads), 0, s, a, tiles_t, tiles_n);
-    else
-      hipLaunchKernelGGL(int8_tile_kernel<false>, dim3(tiles_t * tiles_n), dim3(kTileThreads), 0, s, a, tiles_t, tiles_n);
+  if (a.tokens <= kFewTokens) {
+    const FewPlan p = few_plan(a.tokens, a.k, a.n);
+    if (a.tokens <= 16 && p.channels == 16) launch_few<1, 1, 2, 8>(a, p, s);
+    else if (a.tokens <= 16) launch_few<1, 2, 1, 4>(a, p, s);
+    else if (a.tokens <= 32) launch_few<2, 2, 2, 4>(a, p, s);
+    else launch_few<4, 4, 1, 4>(a, p, s);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL(int8_kernel, dim3((unsigned)(((a.n + 63) / 64) * ((a.tokens + 63) / 64))),
-                     dim3(256), 0, s, a);
+  const int tiles_t = (int)((a.tokens + kTile - 1) / kTile), tiles_n = (int)((a.n + kTile - 1) / kTile);
+  const dim3 grid(tiles_t * tiles_n), block(kTileThreads);
+  if (a.out_f32 || a.accumulate)
+    hipLaunchKernelGGL(int8_tile_kernel<true>, grid, block, 0, s, a, tiles_t, tiles_n);
+  else
+    hipLaunchKernelGGL(int8_tile_kernel<false>, grid, block, 0, s, a, tiles_t, tiles_n);
   return hipGetLastError();
 }
 
