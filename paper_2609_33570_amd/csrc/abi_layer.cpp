@@ -235,7 +235,18 @@ hilore_status check_states(const hilore_adamw_tensor *t, int n) {
   return HILORE_OK;
 }
 
-int64_t norm_chunks(int64_t n) { return (n + hilore::kNormChunk - 1) / hilore::kNormChunk; }
+int64_t norm_chunks(const hilore_adamw_tensor &t) {
+  const int64_t elems = hilore::kNormChunkBytes / (t.grad_bf16 ? 2 : 4);
+  return (t.n + elems - 1) / elems;
+}
+
+// Empties a launch's batch of tensors.
+template <typename Batch>
+void clear(Batch &b, int &count) {
+  count = 0;
+  b.chunks = 0;
+  for (uint32_t &x : b.begin) x = ~0u;
+}
 
 }  // namespace
 
@@ -356,7 +367,7 @@ hilore_status hilore_quantize_tokens(const uint16_t *x, const float *factor, int
 size_t hilore_grad_norm_workspace_bytes(const hilore_adamw_tensor *tensors, int n_tensors) {
   if (check_gradients(tensors, n_tensors) != HILORE_OK) return 0;
   int64_t chunks = 0;
-  for (int i = 0; i < n_tensors; ++i) chunks += norm_chunks(tensors[i].n);
+  for (int i = 0; i < n_tensors; ++i) chunks += norm_chunks(tensors[i]);
   return (size_t)chunks * sizeof(double);
 }
 
@@ -374,27 +385,29 @@ hilore_status hilore_grad_norm(const hilore_adamw_tensor *tensors, int n_tensors
   hipStream_t s = static_cast<hipStream_t>(stream);
   double *part = static_cast<double *>(workspace);
   int64_t done = 0;
+  int count = 0;
   hilore::NormBatch b{};
+  clear(b, count);
   auto flush = [&]() -> hilore_status {
-    if (b.n == 0) return HILORE_OK;
+    if (count == 0) return HILORE_OK;
     b.part = part + done;
     const hilore_status fs = hip_status(hilore::launch_norm_partial(b, s));
-    done += b.begin[b.n];
-    b.n = 0;
+    done += b.chunks;
+    clear(b, count);
     return fs;
   };
   for (int i = 0; i < n_tensors; ++i) {
     if (tensors[i].n == 0) continue;
-    const int64_t chunks = norm_chunks(tensors[i].n);
-    if (b.n == hilore::kNormPerLaunch || (b.n > 0 && b.begin[b.n] + chunks > kMaxChunks)) {
+    const int64_t chunks = norm_chunks(tensors[i]);
+    if (count == hilore::kNormPerLaunch || (count > 0 && b.chunks + chunks > kMaxChunks)) {
       const hilore_status fs = flush();
       if (fs != HILORE_OK) return fs;
     }
-    b.t[b.n].grad = tensors[i].grad;
-    b.t[b.n].n = tensors[i].n;
-    b.t[b.n].grad16 = tensors[i].grad_bf16 ? 1 : 0;
-    b.begin[b.n + 1] = b.begin[b.n] + (uint32_t)chunks;
-    ++b.n;
+    b.t[count].grad = tensors[i].grad;
+    b.t[count].n = (uint32_t)tensors[i].n;
+    b.t[count].grad16 = tensors[i].grad_bf16 ? 1 : 0;
+    b.begin[count++] = b.chunks;
+    b.chunks += (uint32_t)chunks;
   }
   const hilore_status fs = flush();
   if (fs != HILORE_OK) return fs;
@@ -415,7 +428,9 @@ hilore_status hilore_adamw(const hilore_adamw_tensor *tensors, int n_tensors, do
   const double c1 = 1.0 - std::pow(beta1, (double)step);
   const double c2 = 1.0 - std::pow(beta2, (double)step);
   hipStream_t s = static_cast<hipStream_t>(stream);
+  int count = 0;
   hilore::AdamwBatch b{};
+  clear(b, count);
   b.norm = norm;
   b.beta1 = (float)beta1;
   b.one_beta1 = (float)(1.0 - beta1);
@@ -427,12 +442,12 @@ hilore_status hilore_adamw(const hilore_adamw_tensor *tensors, int n_tensors, do
     const hilore_adamw_tensor &t = tensors[i];
     if (t.n == 0) continue;
     const int64_t chunks = (t.n + hilore::kAdamwChunk - 1) / hilore::kAdamwChunk;
-    if (b.n == hilore::kAdamwPerLaunch || (b.n > 0 && b.begin[b.n] + chunks > kMaxChunks)) {
+    if (count == hilore::kAdamwPerLaunch || (count > 0 && b.chunks + chunks > kMaxChunks)) {
       st = hip_status(hilore::launch_adamw(b, s));
       if (st != HILORE_OK) return st;
-      b.n = 0;
+      clear(b, count);
     }
-    hilore::AdamwTensor &o = b.t[b.n];
+    hilore::AdamwTensor &o = b.t[count];
     o.p = t.p;
     o.p16 = t.p16;
     o.grad = t.grad;
@@ -446,10 +461,10 @@ hilore_status hilore_adamw(const hilore_adamw_tensor *tensors, int n_tensors, do
     o.key_state = hilore::adamw_key(seed, i, 0u);
     o.key_param = hilore::adamw_key(seed, i, 0x3C6EF372u);
     o.grad16 = t.grad_bf16 ? 1 : 0;
-    b.begin[b.n + 1] = b.begin[b.n] + (uint32_t)chunks;
-    ++b.n;
+    b.begin[count++] = b.chunks;
+    b.chunks += (uint32_t)chunks;
   }
-  return b.n > 0 ? hip_status(hilore::launch_adamw(b, s)) : HILORE_OK;
+  return count > 0 ? hip_status(hilore::launch_adamw(b, s)) : HILORE_OK;
 }
 
 }  // extern "C"

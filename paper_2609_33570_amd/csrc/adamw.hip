@@ -25,18 +25,8 @@ namespace hilore {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kLaneElems = 4;                       // consecutive elements of a lane
-constexpr int kBlock = kWave * kLaneElems;          // 256: one state block a wave
-constexpr int kBlocksPerWave = (int)(kAdamwChunk / kThreads / kLaneElems);
-static_assert(kBlock == kAdamwBlock, "a wave owns one state block at a time");
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-// Largest unsigned value of the wave (all lanes receive it).
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-  v = group_max_u32<32>(v);
-  return max(v, (uint32_t)__shfl_xor((int)v, 32, kWave));
-}
 
 __device__ __forceinline__ uint32_t mix32(uint32_t x) {
   x ^= x >> 16;
@@ -46,185 +36,327 @@ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-// Four consecutive elements at p + i, of which `n` exist; the others read as 0.
-__device__ __forceinline__ void load4(const float *p, int64_t i, int n, float v[4]) {
-  if (n >= 4) {
-    const f32x4 w = *reinterpret_cast<const f32x4 *>(p + i);
-    v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+// A lane's E consecutive elements as they lie in memory.  With `n` < E of them the others
+// read as 0 and are not written (FULL: n >= E is known).
+template <typename T, int E>
+struct Lane {
+  static constexpr int kBytes = E * (int)sizeof(T), kWords = kBytes / 4;
+  uint32_t w[kWords];
+};
+
+template <bool FULL, typename T, int E>
+__device__ __forceinline__ void load_lane(Lane<T, E> &v, const T *p, int64_t i, int n) {
+  using L = Lane<T, E>;
+  if (FULL || n >= E) {
+    if constexpr (L::kBytes == 4) {
+      v.w[0] = *reinterpret_cast<const uint32_t *>(p + i);
+    } else if constexpr (L::kBytes == 8) {
+      const u32x2 a = *reinterpret_cast<const u32x2 *>(p + i);
+      v.w[0] = a.x; v.w[1] = a.y;
+    } else {
+#pragma unroll
+      for (int k = 0; k < L::kBytes / 16; ++k) {
+        const u32x4 a = *(reinterpret_cast<const u32x4 *>(p + i) + k);
+        v.w[4 * k] = a.x; v.w[4 * k + 1] = a.y; v.w[4 * k + 2] = a.z; v.w[4 * k + 3] = a.w;
+      }
+    }
   } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = k < n ? p[i + k] : 0.0f;
+    for (int k = 0; k < L::kWords; ++k) v.w[k] = 0;
+#pragma unroll
+    for (int k = 0; k < E; ++k)
+      if (k < n) {
+        constexpr int kPer = 4 / (int)sizeof(T);
+        if constexpr (kPer == 1) v.w[k] = __builtin_bit_cast(uint32_t, p[i + k]);
+        else v.w[k / kPer] |= (uint32_t)p[i + k] << (8 * (int)sizeof(T) * (k % kPer));
+      }
   }
 }
 
-__device__ __forceinline__ void store4(float *p, int64_t i, int n, const float v[4]) {
-  if (n >= 4) {
-    *reinterpret_cast<f32x4 *>(p + i) = f32x4{v[0], v[1], v[2], v[3]};
+template <bool FULL, typename T, int E>
+__device__ __forceinline__ void store_lane(const Lane<T, E> &v, T *p, int64_t i, int n) {
+  using L = Lane<T, E>;
+  if (FULL || n >= E) {
+    if constexpr (L::kBytes == 4) {
+      *reinterpret_cast<uint32_t *>(p + i) = v.w[0];
+    } else if constexpr (L::kBytes == 8) {
+      *reinterpret_cast<u32x2 *>(p + i) = u32x2{v.w[0], v.w[1]};
+    } else {
+#pragma unroll
+      for (int k = 0; k < L::kBytes / 16; ++k)
+        *(reinterpret_cast<u32x4 *>(p + i) + k) =
+            u32x4{v.w[4 * k], v.w[4 * k + 1], v.w[4 * k + 2], v.w[4 * k + 3]};
+    }
   } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k < n) p[i + k] = v[k];
+    for (int k = 0; k < E; ++k)
+      if (k < n) {
+        constexpr int kPer = 4 / (int)sizeof(T);
+        if constexpr (kPer == 1) p[i + k] = __builtin_bit_cast(T, v.w[k]);
+        else p[i + k] = (T)(v.w[k / kPer] >> (8 * (int)sizeof(T) * (k % kPer)));
+      }
   }
 }
 
-__device__ __forceinline__ void load4(const uint16_t *p, int64_t i, int n, float v[4]) {
-  if (n >= 4) {
-    const u32x2 w = *reinterpret_cast<const u32x2 *>(p + i);
-    v[0] = bf16_lo(w.x); v[1] = bf16_hi(w.x);
-    v[2] = bf16_lo(w.y); v[3] = bf16_hi(w.y);
-  } else {
+template <int E>
+__device__ __forceinline__ void values(const Lane<float, E> &l, float v[E]) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = k < n ? __uint_as_float((uint32_t)p[i + k] << 16) : 0.0f;
+  for (int k = 0; k < E; ++k) v[k] = __uint_as_float(l.w[k]);
+}
+
+template <int E>
+__device__ __forceinline__ void values(const Lane<uint16_t, E> &l, float v[E]) {
+#pragma unroll
+  for (int k = 0; k < E; k += 2) {
+    v[k] = bf16_lo(l.w[k / 2]);
+    v[k + 1] = bf16_hi(l.w[k / 2]);
   }
 }
 
-__device__ __forceinline__ void store4_bf16(uint16_t *p, int64_t i, int n, uint32_t lo,
-                                            uint32_t hi) {
-  if (n >= 4) {
-    *reinterpret_cast<u32x2 *>(p + i) = u32x2{lo, hi};
-  } else {
-    if (n > 0) p[i] = (uint16_t)lo;
-    if (n > 1) p[i + 1] = (uint16_t)(lo >> 16);
-    if (n > 2) p[i + 2] = (uint16_t)hi;
+// E4M3FN codes times their block's scale.
+template <int E>
+__device__ __forceinline__ void decode(const Lane<uint8_t, E> &l, float s, float v[E]) {
+#pragma unroll
+  for (int k = 0; k < E; k += 4) {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)l.w[k / 4], false);
+    const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8((int)l.w[k / 4], true);
+    v[k] = a.x * s; v[k + 1] = a.y * s; v[k + 2] = b.x * s; v[k + 3] = b.y * s;
   }
 }
 
-__device__ __forceinline__ uint32_t load4_codes(const uint8_t *p, int64_t i, int n) {
-  if (n >= 4) return *reinterpret_cast<const uint32_t *>(p + i);
-  uint32_t w = 0;
+// Codes of a block's values (E of 256 in each lane) with 16 random bits each, and the block's
+// scale.  KEEP: x >= 0, and what is above zero stays above it.  BIG: blocks up to fp32's
+// largest; else up to 2^12, where 448 / amax 2^-120 is a normal number.
+template <bool KEEP, bool BIG, int E>
+__device__ __forceinline__ void encode(const float x[E], const uint32_t bits[E], float amax,
+                                       Lane<uint8_t, E> &out, float &scale) {
+  const bool none = amax < 0x1p-64f;
+  float inv;
+  if constexpr (BIG) {
+    inv = 1.0f / amax;
+  } else {  // one Newton step after the hardware's
+    inv = __builtin_amdgcn_rcpf(amax);
+    inv = fmaf(fmaf(-amax, inv, 1.0f), inv, inv);
+  }
+  scale = none ? 0.0f : amax * (1.0f / 448.0f);
+  const float r = none ? 0.0f : (448.0f * inv) * (BIG ? 1.0f : 0x1p-120f);
+  const uint32_t least = none ? 0u : 1u;
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (k < n) w |= (uint32_t)p[i + k] << (8 * k);
-  return w;
-}
-
-__device__ __forceinline__ void store4_codes(uint8_t *p, int64_t i, int n, uint32_t w) {
-  if (n >= 4) {
-    *reinterpret_cast<uint32_t *>(p + i) = w;
-  } else {
+  for (int k = 0; k < E; k += 4) {
+    uint32_t c[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k < n) p[i + k] = (uint8_t)(w >> (8 * k));
+    for (int e = 0; e < 4; ++e) {
+      float y = fabsf(x[k + e]) * r;
+      if constexpr (BIG) y *= 0x1p-120f;
+      const uint32_t u = ((bits[k + e] << 4) + __float_as_uint(y)) >> 20;
+      const uint32_t low = KEEP ? min(__float_as_uint(x[k + e]), least) : 0u;
+      c[e] = max(min(u, 0x7Eu), low);
+    }
+    uint32_t w = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+    if constexpr (!KEEP) {  // the signs: the four upper bytes' top bits
+      const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(x[k + 1]), __float_as_uint(x[k]), 0x0C0C0703u);
+      const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(x[k + 3]), __float_as_uint(x[k + 2]), 0x07030C0Cu);
+      w |= (lo | hi) & 0x80808080u;
+    }
+    out.w[k / 4] = w;
   }
 }
 
-__device__ __forceinline__ void decode4(uint32_t c, float s, float v[4]) {
-  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false);
-  const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
-  v[0] = a.x * s; v[1] = a.y * s; v[2] = b.x * s; v[3] = b.y * s;
-}
-
-// Codes of a block's values (this lane's 4) with 16 random bits each, and its scale.
-template <bool KEEP>
-__device__ __forceinline__ uint32_t encode4(const float x[4], const uint32_t bits[4], float &scale) {
+template <int E>
+__device__ __forceinline__ float block_amax(const float x[E]) {
   uint32_t top = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) top = max(top, __float_as_uint(fabsf(x[k])));
-  const float amax = __uint_as_float(wave_max_u32(top));
-  const bool none = amax < 0x1p-64f;
-  scale = none ? 0.0f : amax * (1.0f / 448.0f);
-  const float r = none ? 0.0f : 448.0f * (1.0f / amax);
-  uint32_t w = 0;
+  for (int k = 0; k < E; ++k) top = max(top, __float_as_uint(fabsf(x[k])));
+  return __uint_as_float(lanes_max_u32<256 / E>(top));
+}
+
+// Roots of v >= 0: a Newton step after the hardware's reciprocal root, which is for normal
+// numbers (the library's sqrtf, three times as long, for the others).
+template <int E>
+__device__ __forceinline__ void roots(const float v[E], float r[E]) {
+  bool other = false;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float a = fabsf(x[k]) * r * 0x1p-120f;
-    uint32_t c = min((__float_as_uint(a) + (bits[k] << 4)) >> 20, 0x7Eu);
-    if constexpr (KEEP) c = x[k] > 0.0f && !none ? max(c, 1u) : c;
-    else c |= (__float_as_uint(x[k]) >> 24) & 0x80u;
-    w |= c << (8 * k);
+  for (int k = 0; k < E; ++k) {
+    const float y = __builtin_amdgcn_rsqf(fmaxf(v[k], 0x1p-126f));
+    const float s = v[k] * y;
+    r[k] = fmaf(fmaf(-s, s, v[k]), 0.5f * y, s);
+    other |= __builtin_amdgcn_classf(v[k], 0x3 | 0x200 | 0x80 | 0x10);  // NaN, infinity, subnormal
   }
-  return w;
+  if (other) {
+#pragma unroll
+    for (int k = 0; k < E; ++k) r[k] = sqrtf(v[k]);
+  }
 }
 
 struct Scalars {
-  float beta1, one_beta1, beta2, one_beta2, eps, inv_sqrt_c2;
+  float beta1, one_beta1, beta2, one_beta2, eps, inv_sqrt_c2, clip;
 };
 
-// One chunk of one tensor.  PARAM: 0 fp32, 1 fp32 with a bf16 copy, 2 bf16.
+// The elements that a workgroup takes at once: 4 a lane with 32-bit states, 8 with 8-bit
+// ones (a block is then half a wave), which makes the narrow operands' loads 8 and 16 bytes.
 template <bool EIGHT, bool GRAD16, int PARAM>
-__device__ __forceinline__ void step_chunk(const AdamwTensor &t, int64_t begin, float clip,
-                                           const Scalars &s) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  for (int b = 0; b < kBlocksPerWave; ++b) {
-    const int64_t block = begin / kBlock + b * (kThreads / kWave) + wave;
-    const int64_t i = block * kBlock + lane * kLaneElems;
-    if (block * kBlock >= t.n) return;  // the whole wave
-    const int64_t left = t.n - i;
-    const int n = left >= 4 ? 4 : left > 0 ? (int)left : 0;
-    float p[4], g[4], m[4], v[4], r[4];
-    if constexpr (PARAM == 2) load4(t.p16, i, n, p);
-    else load4(t.p, i, n, p);
-    if constexpr (GRAD16) load4(static_cast<const uint16_t *>(t.grad), i, n, g);
-    else load4(static_cast<const float *>(t.grad), i, n, g);
-    if constexpr (EIGHT) {
-      const uint32_t mc = load4_codes(static_cast<const uint8_t *>(t.m), i, n);
-      const uint32_t vc = load4_codes(static_cast<const uint8_t *>(t.v), i, n);
-      decode4(mc, t.m_scales[block], m);
-      decode4(vc, t.v_scales[block], r);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = r[k] * r[k];
-    } else {
-      load4(static_cast<const float *>(t.m), i, n, m);
-      load4(static_cast<const float *>(t.v), i, n, v);
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float gk = g[k] * clip;
-      m[k] = s.beta1 * m[k] + s.one_beta1 * gk;
-      v[k] = s.beta2 * v[k] + s.one_beta2 * (gk * gk);
-      r[k] = sqrtf(v[k]);
-      // rcp is within 1 ulp; eps keeps its operand a normal number
-      p[k] = p[k] * t.decay -
-             (t.step_size * m[k]) * __builtin_amdgcn_rcpf(r[k] * s.inv_sqrt_c2 + s.eps);
-    }
-    if constexpr (EIGHT) {
-      uint32_t lo[4], hi[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t w = mix32((uint32_t)(i + k) ^ t.key_state);
-        lo[k] = w & 0xFFFFu;
-        hi[k] = w >> 16;
-      }
-      float ms, vs;
-      const uint32_t mc = encode4<false>(m, lo, ms);
-      const uint32_t vc = encode4<true>(r, hi, vs);
-      store4_codes(static_cast<uint8_t *>(t.m), i, n, mc);
-      store4_codes(static_cast<uint8_t *>(t.v), i, n, vc);
-      if (lane == 0) {
-        t.m_scales[block] = ms;
-        t.v_scales[block] = vs;
-      }
-    } else {
-      store4(static_cast<float *>(t.m), i, n, m);
-      store4(static_cast<float *>(t.v), i, n, v);
-    }
-    if constexpr (PARAM != 2) store4(t.p, i, n, p);
-    if constexpr (PARAM == 1)
-      store4_bf16(t.p16, i, n, pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]));
-    if constexpr (PARAM == 2) {
-      uint32_t w[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        // NaN and infinity have no bits to round
-        const uint32_t u = __float_as_uint(p[k]);
-        const uint32_t q = mix32((uint32_t)(i + k) ^ t.key_param) & 0xFFFFu;
-        w[k] = (u & 0x7F800000u) == 0x7F800000u ? u | ((u & 0xFFFFu) ? 0x10000u : 0u) : u + q;
-      }
-      store4_bf16(t.p16, i, n, (w[0] >> 16) | (w[1] & 0xFFFF0000u),
-                  (w[2] >> 16) | (w[3] & 0xFFFF0000u));
-    }
+struct Piece {
+  static constexpr int E = EIGHT ? 8 : 4;
+  Lane<float, E> p, m, v;
+  Lane<uint16_t, E> p16;
+  Lane<float, E> g;
+  Lane<uint16_t, E> g16;
+  Lane<uint8_t, E> mc, vc;
+  float ms, vs;
+};
+
+template <bool FULL, bool EIGHT, bool GRAD16, int PARAM>
+__device__ __forceinline__ void load_piece(Piece<EIGHT, GRAD16, PARAM> &x, const AdamwTensor &t,
+                                           int64_t i, int n) {
+  if constexpr (PARAM == 2) load_lane<FULL>(x.p16, (const uint16_t *)t.p16, i, n);
+  else load_lane<FULL>(x.p, (const float *)t.p, i, n);
+  if constexpr (GRAD16) load_lane<FULL>(x.g16, static_cast<const uint16_t *>(t.grad), i, n);
+  else load_lane<FULL>(x.g, static_cast<const float *>(t.grad), i, n);
+  if constexpr (EIGHT) {
+    load_lane<FULL>(x.mc, static_cast<const uint8_t *>(t.m), i, n);
+    load_lane<FULL>(x.vc, static_cast<const uint8_t *>(t.v), i, n);
+    const int64_t block = FULL || n > 0 ? i / kAdamwBlock : 0;
+    x.ms = t.m_scales[block];
+    x.vs = t.v_scales[block];
+  } else {
+    load_lane<FULL>(x.m, static_cast<const float *>(t.m), i, n);
+    load_lane<FULL>(x.v, static_cast<const float *>(t.v), i, n);
   }
 }
 
-// Tensor of workgroup `b`: the last one whose chunks begin at or before it.
-__device__ __forceinline__ int tensor_of(const uint32_t *begin, int n, int64_t b) {
-  int lo = 0, hi = n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (begin[mid] <= b) lo = mid;
-    else hi = mid - 1;
+// One step of a piece.  PARAM: 0 fp32, 1 fp32 with a bf16 copy, 2 bf16.
+template <bool FULL, bool EIGHT, bool GRAD16, int PARAM>
+__device__ __forceinline__ void step_piece(Piece<EIGHT, GRAD16, PARAM> &x, const AdamwTensor &t,
+                                           int64_t i, int n, const Scalars &s) {
+  constexpr int E = Piece<EIGHT, GRAD16, PARAM>::E;
+  float p[E], g[E], m[E], v[E], r[E];
+  if constexpr (PARAM == 2) values(x.p16, p);
+  else values(x.p, p);
+  if constexpr (GRAD16) values(x.g16, g);
+  else values(x.g, g);
+  if constexpr (EIGHT) {
+    decode(x.mc, x.ms, m);
+    decode(x.vc, x.vs, r);
+#pragma unroll
+    for (int k = 0; k < E; ++k) v[k] = r[k] * r[k];
+  } else {
+    values(x.m, m);
+    values(x.v, v);
   }
-  return lo;
+#pragma unroll
+  for (int k = 0; k < E; ++k) {
+    const float gk = g[k] * s.clip;
+    m[k] = s.beta1 * m[k] + s.one_beta1 * gk;
+    v[k] = s.beta2 * v[k] + s.one_beta2 * (gk * gk);
+  }
+  roots<E>(v, r);
+#pragma unroll
+  for (int k = 0; k < E; ++k)  // rcp is within 1 ulp; eps keeps its operand a normal number
+    p[k] = p[k] * t.decay -
+           (t.step_size * m[k]) * __builtin_amdgcn_rcpf(r[k] * s.inv_sqrt_c2 + s.eps);
+  if constexpr (EIGHT) {
+    uint32_t lo[E], hi[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      const uint32_t w = mix32((uint32_t)(i + k) ^ t.key_state);
+      lo[k] = w & 0xFFFFu;
+      hi[k] = w >> 16;
+    }
+    const float am = block_amax<E>(m), ar = block_amax<E>(r);
+    if (__builtin_expect(__any(!(am <= 0x1p12f) || !(ar <= 0x1p12f)), 0)) {
+      encode<false, true, E>(m, lo, am, x.mc, x.ms);
+      encode<true, true, E>(r, hi, ar, x.vc, x.vs);
+    } else {
+      encode<false, false, E>(m, lo, am, x.mc, x.ms);
+      encode<true, false, E>(r, hi, ar, x.vc, x.vs);
+    }
+    store_lane<FULL>(x.mc, static_cast<uint8_t *>(t.m), i, n);
+    store_lane<FULL>(x.vc, static_cast<uint8_t *>(t.v), i, n);
+    if ((threadIdx.x & (kAdamwBlock / E - 1)) == 0 && (FULL || n > 0)) {
+      t.m_scales[i / kAdamwBlock] = x.ms;
+      t.v_scales[i / kAdamwBlock] = x.vs;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      x.m.w[k] = __float_as_uint(m[k]);
+      x.v.w[k] = __float_as_uint(v[k]);
+    }
+    store_lane<FULL>(x.m, static_cast<float *>(t.m), i, n);
+    store_lane<FULL>(x.v, static_cast<float *>(t.v), i, n);
+  }
+  if constexpr (PARAM != 2) {
+#pragma unroll
+    for (int k = 0; k < E; ++k) x.p.w[k] = __float_as_uint(p[k]);
+    store_lane<FULL>(x.p, t.p, i, n);
+  }
+  if constexpr (PARAM == 1) {
+#pragma unroll
+    for (int k = 0; k < E; k += 2) x.p16.w[k / 2] = pack_bf16(p[k], p[k + 1]);
+    store_lane<FULL>(x.p16, t.p16, i, n);
+  }
+  if constexpr (PARAM == 2) {
+    uint32_t w[E];
+    bool other = false;
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      w[k] = __float_as_uint(p[k]) + (mix32((uint32_t)(i + k) ^ t.key_param) & 0xFFFFu);
+      other |= __builtin_amdgcn_classf(p[k], 0x3 | 0x200 | 0x4);
+    }
+    if (other) {  // NaN and infinity have no bits to round
+#pragma unroll
+      for (int k = 0; k < E; ++k)
+        if (__builtin_amdgcn_classf(p[k], 0x3 | 0x200 | 0x4))
+          w[k] = __float_as_uint(p[k]) | (p[k] != p[k] ? 0x400000u : 0u);
+    }
+#pragma unroll
+    for (int k = 0; k < E; k += 2) x.p16.w[k / 2] = __builtin_amdgcn_perm(w[k + 1], w[k], 0x07060302u);
+    store_lane<FULL>(x.p16, t.p16, i, n);
+  }
+}
+
+// One chunk of one tensor: every load goes out before the first step.
+template <bool FULL, bool EIGHT, bool GRAD16, int PARAM>
+__device__ __forceinline__ void step_chunk(const AdamwTensor &t, int64_t begin, const Scalars &s) {
+  constexpr int E = Piece<EIGHT, GRAD16, PARAM>::E;
+  constexpr int kPieces = (int)kAdamwChunk / kThreads / E;
+  Piece<EIGHT, GRAD16, PARAM> x[kPieces];
+  const int64_t first = begin + (int64_t)threadIdx.x * E;
+  const auto count = [&](int64_t i) {
+    const int64_t left = t.n - i;
+    return left >= E ? E : left > 0 ? (int)left : 0;
+  };
+#pragma unroll
+  for (int k = 0; k < kPieces; ++k) {
+    const int64_t i = first + k * kThreads * E;
+    load_piece<FULL>(x[k], t, i, FULL ? E : count(i));
+  }
+#pragma unroll
+  for (int k = 0; k < kPieces; ++k) {
+    const int64_t i = first + k * kThreads * E;
+    step_piece<FULL>(x[k], t, i, FULL ? E : count(i), s);
+  }
+}
+
+template <bool EIGHT, bool GRAD16, int PARAM>
+__device__ __forceinline__ void step_any(const AdamwTensor &t, int64_t begin, const Scalars &s) {
+  if (begin + kAdamwChunk <= t.n) step_chunk<true, EIGHT, GRAD16, PARAM>(t, begin, s);
+  else step_chunk<false, EIGHT, GRAD16, PARAM>(t, begin, s);
+}
+
+// Tensor of workgroup `b`: the last whose chunks begin at or before it (unused entries of
+// `begin` are 2^32 - 1).  Every lane looks at one tensor of 64, so there is one load's wait,
+// where a binary search has one a step (233M elements, 8 bit: 560 -> 430 us with the step's
+// instructions cut; by unrolled scalar loads 463).
+template <int N>
+__device__ __forceinline__ int tensor_of(const uint32_t *begin, uint32_t b) {
+  int before = 0;
+#pragma unroll
+  for (int j = 0; j < N; j += kWave) {
+    const int i = j + (int)(threadIdx.x & 63);
+    before += __popcll(__ballot(i < N && begin[i < N ? i : 0] <= b));
+  }
+  return before - 1;
 }
 
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwBatch a) {
@@ -233,25 +365,26 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwBatch a) {
     clip = a.norm[1];
     if (!(clip <= 1.0f)) return;  // NaN: the step is skipped
   }
-  const int k = tensor_of(a.begin, a.n, blockIdx.x);
+  const int k = tensor_of<kAdamwPerLaunch>(a.begin, blockIdx.x);
   const AdamwTensor &t = a.t[k];
   const int64_t begin = ((int64_t)blockIdx.x - a.begin[k]) * kAdamwChunk;
-  const Scalars s = {a.beta1, a.one_beta1, a.beta2, a.one_beta2, a.eps, a.inv_sqrt_c2};
+  const Scalars s = {a.beta1, a.one_beta1, a.beta2,
+                     a.one_beta2, a.eps, a.inv_sqrt_c2, clip};
   const int param = t.p ? (t.p16 ? 1 : 0) : 2;
   const int kind = (t.m_scales ? 6 : 0) + (t.grad16 ? 3 : 0) + param;
   switch (kind) {
-    case 0: return step_chunk<false, false, 0>(t, begin, clip, s);
-    case 1: return step_chunk<false, false, 1>(t, begin, clip, s);
-    case 2: return step_chunk<false, false, 2>(t, begin, clip, s);
-    case 3: return step_chunk<false, true, 0>(t, begin, clip, s);
-    case 4: return step_chunk<false, true, 1>(t, begin, clip, s);
-    case 5: return step_chunk<false, true, 2>(t, begin, clip, s);
-    case 6: return step_chunk<true, false, 0>(t, begin, clip, s);
-    case 7: return step_chunk<true, false, 1>(t, begin, clip, s);
-    case 8: return step_chunk<true, false, 2>(t, begin, clip, s);
-    case 9: return step_chunk<true, true, 0>(t, begin, clip, s);
-    case 10: return step_chunk<true, true, 1>(t, begin, clip, s);
-    default: return step_chunk<true, true, 2>(t, begin, clip, s);
+    case 0: return step_any<false, false, 0>(t, begin, s);
+    case 1: return step_any<false, false, 1>(t, begin, s);
+    case 2: return step_any<false, false, 2>(t, begin, s);
+    case 3: return step_any<false, true, 0>(t, begin, s);
+    case 4: return step_any<false, true, 1>(t, begin, s);
+    case 5: return step_any<false, true, 2>(t, begin, s);
+    case 6: return step_any<true, false, 0>(t, begin, s);
+    case 7: return step_any<true, false, 1>(t, begin, s);
+    case 8: return step_any<true, false, 2>(t, begin, s);
+    case 9: return step_any<true, true, 0>(t, begin, s);
+    case 10: return step_any<true, true, 1>(t, begin, s);
+    default: return step_any<true, true, 2>(t, begin, s);
   }
 }
 
@@ -268,24 +401,38 @@ __device__ __forceinline__ double group_sum(double v, double *lds) {
 }
 
 // Sum of squares of one chunk of one gradient, in fp64 (an fp32 square would
-// overflow from 2^64 on and vanish below 2^-75).
+// overflow from 2^64 on and vanish below 2^-75).  All of a thread's loads go out first.
+template <bool FULL, typename T>
+__device__ __forceinline__ double chunk_squares(const T *g, int64_t n, int64_t begin) {
+  constexpr int E = 16 / (int)sizeof(T), kLoads = (int)(kNormChunkBytes / kThreads / 16);
+  Lane<T, E> x[kLoads];
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const int64_t i = begin + (j * kThreads + (int)threadIdx.x) * E, left = n - i;
+    load_lane<FULL>(x[j], g, i, left >= E ? E : left > 0 ? (int)left : 0);
+  }
+  double sum = 0.0;
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    float v[E];
+    values(x[j], v);
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum = fma((double)v[e], (double)v[e], sum);
+  }
+  return sum;
+}
+
 __global__ __launch_bounds__(kThreads) void norm_partial_kernel(const NormBatch a) {
   __shared__ double lds[kThreads / kWave];
-  const int k = tensor_of(a.begin, a.n, blockIdx.x);
+  const int k = tensor_of<kNormPerLaunch>(a.begin, blockIdx.x);
   const NormTensor &t = a.t[k];
-  const int64_t begin = ((int64_t)blockIdx.x - a.begin[k]) * kNormChunk;
-  double sum = 0.0;
-#pragma unroll 4
-  for (int j = 0; j < (int)(kNormChunk / kThreads / 4); ++j) {
-    const int64_t i = begin + (j * kThreads + (int)threadIdx.x) * 4;
-    const int64_t left = t.n - i;
-    const int n = left >= 4 ? 4 : left > 0 ? (int)left : 0;
-    float g[4];
-    if (t.grad16) load4(static_cast<const uint16_t *>(t.grad), i, n, g);
-    else load4(static_cast<const float *>(t.grad), i, n, g);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sum = fma((double)g[e], (double)g[e], sum);
-  }
+  const int64_t chunk = kNormChunkBytes / (t.grad16 ? 2 : 4);  // elements
+  const int64_t begin = ((int64_t)blockIdx.x - a.begin[k]) * chunk, n = t.n;
+  const bool full = begin + chunk <= n;
+  const float *g = static_cast<const float *>(t.grad);
+  const uint16_t *g16 = static_cast<const uint16_t *>(t.grad);
+  double sum = t.grad16 ? (full ? chunk_squares<true>(g16, n, begin) : chunk_squares<false>(g16, n, begin))
+                        : (full ? chunk_squares<true>(g, n, begin) : chunk_squares<false>(g, n, begin));
   sum = group_sum(sum, lds);
   if (threadIdx.x == 0) a.part[blockIdx.x] = sum;
 }
@@ -296,6 +443,7 @@ __global__ __launch_bounds__(kFoldThreads) void norm_fold_kernel(const double *p
                                                                  float max_norm, float *norm) {
   __shared__ double lds[kFoldThreads / kWave];
   double sum = 0.0;
+#pragma unroll 8
   for (int64_t i = threadIdx.x; i < n; i += kFoldThreads) sum += part[i];
   sum = group_sum(sum, lds);
   if (threadIdx.x == 0) {
@@ -314,12 +462,12 @@ __global__ __launch_bounds__(kFoldThreads) void norm_fold_kernel(const double *p
 }  // namespace
 
 hipError_t launch_adamw(const AdamwBatch &a, hipStream_t s) {
-  hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)a.begin[a.n]), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(adamw_kernel, dim3(a.chunks), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_norm_partial(const NormBatch &a, hipStream_t s) {
-  hipLaunchKernelGGL(norm_partial_kernel, dim3((unsigned)a.begin[a.n]), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(norm_partial_kernel, dim3(a.chunks), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -122,6 +122,41 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// The value that a DPP control brings to the lane (the controls above have a source for
+// every lane).
+template <int CTRL>
+__device__ __forceinline__ float dpp_f32(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+
+// Largest unsigned value over aligned groups of 32 (L = 32) or all 64 lanes, all of them
+// receiving it, without LDS instructions: DPP within rows of 16, then the rows swapped in
+// pairs, then the halves.
+template <int L>
+__device__ __forceinline__ uint32_t lanes_max_u32(uint32_t v) {
+  static_assert(L == 32 || L == 64, "group size");
+  v = group_max_u32<16>(v);
+  auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(p[0], p[1]);
+  if constexpr (L == 64) {
+    p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = max(p[0], p[1]);
+  }
+  return v;
+}
+
+// wave_sum's tree, and so its bits, without LDS instructions.
+__device__ __forceinline__ float lanes_sum(float v) {
+  v += dpp_f32<kDppQuadXor1>(v);
+  v += dpp_f32<kDppQuadXor2>(v);
+  v += dpp_f32<kDppRowHalfMirror>(v);
+  v += dpp_f32<kDppRowMirror>(v);
+  auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
 // Rounding of a token's values to int8: the factor 127 / amax and the scale amax / 127.
 // Below 2^-64 both are 0; an infinite or NaN amax gives factor 0 and scale NaN.
 __device__ __forceinline__ float token_scale(float amax, float &scale) {

@@ -295,8 +295,8 @@ struct AdamwTensor {
 };
 struct AdamwBatch {
   AdamwTensor t[kAdamwPerLaunch];
-  uint32_t begin[kAdamwPerLaunch + 1];  // prefix sum of the tensors' chunks
-  int n;
+  uint32_t begin[kAdamwPerLaunch];  // first chunk of each tensor, then 2^32 - 1
+  uint32_t chunks;
   const float *norm;
   float beta1, one_beta1, beta2, one_beta2, eps, inv_sqrt_c2;
 };
@@ -304,17 +304,17 @@ static_assert(sizeof(AdamwBatch) <= 4096, "kernel arguments");
 hipError_t launch_adamw(const AdamwBatch &a, hipStream_t s);
 uint32_t adamw_key(uint32_t seed, int index, uint32_t salt);
 
-constexpr int64_t kNormChunk = 16384;     // elements per workgroup
-constexpr int kNormPerLaunch = 128;
+constexpr int64_t kNormChunkBytes = 32768;  // of a gradient per workgroup
+constexpr int kNormPerLaunch = 192;
 struct NormTensor {
   const void *grad;
-  int64_t n;
-  int64_t grad16;
+  uint32_t n;  // < 2^32
+  uint32_t grad16;
 };
 struct NormBatch {
   NormTensor t[kNormPerLaunch];
-  uint32_t begin[kNormPerLaunch + 1];
-  int n;
+  uint32_t begin[kNormPerLaunch];
+  uint32_t chunks;
   double *part;  // partial sums of this launch's chunks
 };
 static_assert(sizeof(NormBatch) <= 4096, "kernel arguments");
