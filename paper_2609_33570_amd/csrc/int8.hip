@@ -141,11 +141,14 @@ __device__ __forceinline__ void barrier_but_vmcnt() {
 constexpr int kSlots = 4;
 
 // Rows of one slot: 16 NB channels, then 16 TB tokens, 64 G bytes each; 16-byte chunk c of row
-// r lies at c ^ swz(r), so that a fragment read's 8 lanes of a cycle, on 8 rows, meet all banks.
+// r lies at c ^ swz(r).  A 16-byte read serves 16 lanes a cycle, quads 0, 3, 5, 6 of each half
+// wave and then 1, 2, 4, 7: rows 0..3 and 12..15 at one chunk and 4..11 at the next, or the
+// reverse.  With these swz all 16 meet different banks.
 template <int G>
 __device__ __forceinline__ int few_swz(int row) {
   static_assert(G == 1 || G == 2, "bytes of a row in a slot");
-  return G == 1 ? (row >> 1) & 3 : row & 7;
+  return G == 1 ? (0x78 >> (2 * ((row >> 2) & 3))) & 3  // 0, 2, 3, 1 for rows 0-3, 4-7, 8-11, 12-15
+                : (row & 2) | ((row >> 1) & 4);
 }
 
 template <int TB, int NB, int G>
@@ -155,22 +158,24 @@ struct FewLoad {
   static constexpr int kSlotBytes = kLoads * 1024;
   uint32_t first;  // the lane's row of load 0, times k
   uint32_t step;   // kRows k
-  int chunk;       // the lane's first byte within a slot's k
+  int chunk[2];    // the lane's first byte within a slot's k, in even and odd loads
 };
 
 template <int TB, int NB, int G>
 __device__ __forceinline__ void dma_few(const FewLoad<TB, NB, G> &f, __amdgpu_buffer_rsrc_t rw,
                                         __amdgpu_buffer_rsrc_t rx, int k, int end, uint8_t *slot) {
-  const int kk = k + f.chunk;
-  const uint32_t off = kk < end ? f.first + (uint32_t)kk : kOob;
+  uint32_t off[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    off[i] = k + f.chunk[i] < end ? f.first + (uint32_t)(k + f.chunk[i]) : kOob;
 #pragma unroll
   for (int j = 0; j < NB * G; ++j)
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void *)(slot + j * 1024), 16,
-                                             (int)(off + j * f.step), 0, 0, 0);
+                                             (int)(off[j & 1] + j * f.step), 0, 0, 0);
 #pragma unroll
   for (int j = 0; j < TB * G; ++j)
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void *)(slot + (NB * G + j) * 1024), 16,
-                                             (int)(off + j * f.step), 0, 0, 0);
+                                             (int)(off[j & 1] + j * f.step), 0, 0, 0);
 }
 
 // The products of one slot; `at`: the lane's fragment offset of each k-step of 64.
@@ -237,7 +242,9 @@ __global__ __launch_bounds__(WAVES * 64) void int8_few_kernel(const Int8Args a, 
     const int row = lane / (4 * G);
     f.first = (uint32_t)row * (uint32_t)a.k;
     f.step = (uint32_t)Load::kRows * (uint32_t)a.k;
-    f.chunk = ((lane & (4 * G - 1)) ^ few_swz<G>(row)) * 16;  // kRows % 8 == 0: the same in all loads
+#pragma unroll
+    for (int i = 0; i < 2; ++i)  // 16 rows are one load (G = 1) or two
+      f.chunk[i] = ((lane & (4 * G - 1)) ^ few_swz<G>((row + i * Load::kRows) & 15)) * 16;
   }
   uint32_t at[G];
 #pragma unroll
@@ -307,30 +314,33 @@ __global__ __launch_bounds__(256) void int8_join_kernel(const Int8Args a, int pa
 // 4 x 4 blocks of v_mfma_i32_32x32x32_i8, one wave a SIMD.  Both operands have k
 // contiguous, so they are copied to LDS as they are by the buffer unit (16-byte
 // LDS-DMA loads, no registers) in stages of 64 k: [256 rows][64 B] each, 16-byte
-// chunk g of row r at position g ^ (r / 2 % 4), which spreads the 8 rows that one
+// chunk g of row r at position g ^ (r / 4 % 4), which spreads the 16 rows that one
 // cycle of a fragment read takes over all banks.  Four stages are in flight.
 constexpr int kTile = 256, kStageK = 64, kTileThreads = 256;
 constexpr int kStageBytes = kTile * kStageK;  // of one operand (16 KB)
 constexpr int kStageLoads = 8;                // LDS-DMA instructions of a wave per stage
 constexpr int kGroupT = 8;
+constexpr int kTileGroups = 256;              // one a CU
 
 struct TileLoad {
-  uint32_t a[4], b[4];  // byte offset of the lane's chunk in its row of each load, at k = 0
-  int g16;              // its first k within a stage
+  uint32_t row[4];  // byte offset of the lane's chunk in its row of each load, at k = 0
+  int g16;          // its first k within a stage
+};
+
+struct TileSource {  // the operands' rows of one tile
+  __amdgpu_buffer_rsrc_t a, b;
 };
 
 // Stage k0 of both operands into `la`, `lb`: load r of wave w writes rows 64 w + 16 r ..
 // + 15, lane l the chunk at position l % 4 of row l / 4.  Chunks past k read as 0.
-__device__ __forceinline__ void dma_stage(__amdgpu_buffer_rsrc_t ra, __amdgpu_buffer_rsrc_t rb,
-                                          const TileLoad &tl, int k0, int k, uint8_t *la,
-                                          uint8_t *lb, int wave) {
+__device__ __forceinline__ void dma_stage(const TileSource &src, const TileLoad &tl, int k0, int k,
+                                          uint8_t *la, uint8_t *lb, int wave) {
   const uint32_t past = k0 + tl.g16 < k ? 0u : kOob;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void *)(la + (wave * 64 + r * 16) * kStageK),
-                                             16, (int)((tl.a[r] + (uint32_t)k0) | past), 0, 0, 0);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void *)(lb + (wave * 64 + r * 16) * kStageK),
-                                             16, (int)((tl.b[r] + (uint32_t)k0) | past), 0, 0, 0);
+    const int off = (int)((tl.row[r] + (uint32_t)k0) | past), to = (wave * 64 + r * 16) * kStageK;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src.a, (lds_void *)(la + to), 16, off, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src.b, (lds_void *)(lb + to), 16, off, 0, 0, 0);
   }
 }
 
@@ -387,99 +397,139 @@ __device__ __forceinline__ void schedule16() {
 // fragment reads of stage s + 1.
 __device__ __forceinline__ void tile_stage(i32x16 (&acc)[4][4], TileFrags &f, uint8_t *cur_a,
                                            uint8_t *cur_b, const uint8_t *nxt_a,
-                                           const uint8_t *nxt_b, __amdgpu_buffer_rsrc_t ra,
-                                           __amdgpu_buffer_rsrc_t rb, const TileLoad &tl, int k4,
-                                           int k, const uint32_t (&oa)[2],
-                                           const uint32_t (&ob)[2], int wave) {
+                                           const uint8_t *nxt_b, const TileSource &src,
+                                           const TileLoad &tl, int k4, int k,
+                                           const uint32_t (&oa)[2], const uint32_t (&ob)[2],
+                                           int wave) {
   mma16<0>(acc, f, cur_a, cur_b, oa, ob);
   schedule16<false>();
   barrier_but_vmcnt<2 * kStageLoads>();
-  dma_stage(ra, rb, tl, k4, k, cur_a, cur_b, wave);
+  dma_stage(src, tl, k4, k, cur_a, cur_b, wave);
   mma16<1>(acc, f, nxt_a, nxt_b, oa, ob);
   schedule16<true>();
 }
 
+// One accumulator value, where it is asked for: left to itself the compiler copies all 256 at
+// once and spills what the next tile needs.  (The compiler does not see the read, so its
+// distance from the last MFMA is tile_store's to keep.)
+__device__ __forceinline__ int acc_value(int a) {
+  int v;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(a));
+  return v;
+}
+
+// Scales and bias of one tile in LDS, copied there while the tile before is at work.
+struct TileScales {
+  float sa[kTile], sw[kTile];
+  uint16_t bias[kTile];
+};
+
+__device__ __forceinline__ void dma_scales(const Int8Args &a, int64_t t0, int64_t n0, TileScales &s,
+                                           int wave, int lane) {
+  const int64_t rows_t = a.tokens - t0 < kTile ? a.tokens - t0 : kTile;
+  const int64_t rows_n = a.n - n0 < kTile ? a.n - n0 : kTile;
+  const auto copy = [&](const void *from, int64_t bytes, void *to) {
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(from), 0, (int)bytes, 0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)((uint8_t *)to + wave * 256), 4,
+                                             (wave * 64 + lane) * 4, 0, 0, 0);
+  };
+  copy(a.a_scales + t0, rows_t * 4, s.sa);
+  if (a.w_scales) copy(a.w_scales + n0, rows_n * 4, s.sw);
+  if (a.bias && wave < 2) copy(a.bias + n0, rows_n * 2, s.bias);
+}
+
 // A wave's 128 x 128 outputs.  Accumulator block (i, j): lane l holds token l % 32 of block j
-// and, in register 4 q + e, channel 8 q + 4 (l / 32) + e of block i.  The values go through
-// LDS, [64 tokens][256 B] in `lo` and in `hi` with 16-byte chunk c of a token at c ^ (token %
-// 16), so that rows of the output are written 256 bytes at a time.  WIDE: as fp32, 64 channels
-// at a time (fp32 outputs, and bf16 ones that are added to: one rounding); else as bf16.
+// and, in register 4 q + e, channel 8 q + 4 (l / 32) + e of block i.  The values go through the
+// wave's 4 KB of LDS, 32 tokens of 128 B at a time with 16-byte chunk c of a token at
+// c ^ (token % 8), so that the output is written in whole lines.  WIDE: as fp32, a block of 32
+// channels at a time (fp32 outputs, and bf16 ones that are added to: one rounding); else as
+// bf16, two blocks.
 template <bool WIDE>
 __device__ __forceinline__ void tile_store(const i32x16 (&acc)[4][4], const Int8Args &a,
-                                           uint8_t *lo, uint8_t *hi, int64_t t0, int64_t n0,
-                                           int lane) {
+                                           const TileScales &s, uint8_t *lds, int64_t t0,
+                                           int64_t n0, int wt, int wn, int lane) {
+  constexpr int kBlocks = WIDE ? 1 : 2;
+  asm volatile("s_nop 15\n\ts_nop 15");  // more than the 18 states from an MFMA to a read of its result
+  asm volatile("" : "+v"(lane));  // else the addresses below are formed once and kept, 100 registers
   const int h = lane >> 5, tok = lane & 31;
-  float sa[4];
+  const int c = lane & 7, sub = lane >> 3;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const int64_t t = t0 + j * 32 + tok;
-    sa[j] = t < a.tokens ? a.a_scales[t] : 0.0f;
-  }
+    const float sa = s.sa[wt * 128 + j * 32 + tok];
 #pragma unroll
-  for (int half = 0; half < (WIDE ? 2 : 1); ++half) {
+    for (int i0 = 0; i0 < 4; i0 += kBlocks) {
 #pragma unroll
-    for (int i = WIDE ? 2 * half : 0; i < (WIDE ? 2 * half + 2 : 4); ++i) {
+      for (int i = i0; i < i0 + kBlocks; ++i) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t n = n0 + i * 32 + q * 8 + h * 4;
-        f32x4 sw = {1.0f, 1.0f, 1.0f, 1.0f};
-        float bias[4] = {};
-        if (n < a.n) {
-          if (a.w_scales) sw = *reinterpret_cast<const f32x4 *>(a.w_scales + n);
+        for (int q = 0; q < 4; ++q) {
+          const int at = wn * 128 + i * 32 + q * 8 + h * 4;
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (float)acc_value(acc[i][j][4 * q + e]) * sa;
+          if (a.w_scales) v *= *reinterpret_cast<const f32x4 *>(s.sw + at);
           if (a.bias) {
-            const u32x2 b = *reinterpret_cast<const u32x2 *>(a.bias + n);
-            bias[0] = bf16_lo(b.x); bias[1] = bf16_hi(b.x);
-            bias[2] = bf16_lo(b.y); bias[3] = bf16_hi(b.y);
+            const u32x2 b = *reinterpret_cast<const u32x2 *>(s.bias + at);
+            v += f32x4{bf16_lo(b.x), bf16_hi(b.x), bf16_lo(b.y), bf16_hi(b.y)};
           }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            v[e] = ((float)acc[i][j][4 * q + e] * sa[j]) * sw[e] + bias[e];
-          uint8_t *row = (j < 2 ? lo : hi) + ((j & 1) * 32 + tok) * 256;
+          uint8_t *row = lds + tok * 128;
           if constexpr (WIDE) {
-            const int c = (i & 1) * 8 + q * 2 + h;
-            *reinterpret_cast<f32x4 *>(row + ((c ^ (tok & 15)) << 4)) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4 *>(row + (((q * 2 + h) ^ (tok & 7)) << 4)) = v;
           } else {
-            const int c = i * 4 + q;
-            *reinterpret_cast<u32x2 *>(row + ((c ^ (tok & 15)) << 4) + h * 8) =
-                u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            *reinterpret_cast<u32x2 *>(row + ((((i - i0) * 4 + q) ^ (tok & 7)) << 4) + h * 8) =
+                u32x2{pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)};
           }
         }
       }
-    }
-    // a row of 16 chunks by 16 lanes, 4 rows at a time
-    const int c = lane & 15, sub = lane >> 4;
-#pragma unroll 4
-    for (int it = 0; it < 32; ++it) {
-      const int r = it * 4 + sub;
-      const int64_t t = t0 + r;
-      const u32x4 w = *reinterpret_cast<const u32x4 *>((r < 64 ? lo : hi) + (r & 63) * 256 +
-                                                       ((c ^ (r & 15)) << 4));
-      if (t >= a.tokens) continue;
-      if constexpr (WIDE) {
-        const int64_t n = n0 + half * 64 + c * 4;
-        if (n >= a.n) continue;
-        f32x4 v = __builtin_bit_cast(f32x4, w);
-        if (a.out_f32) {
-          f32x4 *o = reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + t * a.ldo + n);
-          *o = a.accumulate ? *o + v : v;
+      // a row of 8 chunks by 8 lanes, 8 rows at a time
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const int r = it * 8 + sub;
+        const int64_t t = t0 + wt * 128 + j * 32 + r;
+        const int64_t n = n0 + wn * 128 + i0 * 32 + c * (WIDE ? 4 : 8);
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(lds + r * 128 + ((c ^ (r & 7)) << 4));
+        if (t >= a.tokens || n >= a.n) continue;
+        if constexpr (WIDE) {
+          f32x4 v = __builtin_bit_cast(f32x4, w);
+          if (a.out_f32) {
+            f32x4 *o = reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + t * a.ldo + n);
+            *o = a.accumulate ? *o + v : v;
+          } else {
+            u32x2 *o = reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.out) + t * a.ldo + n);
+            const u32x2 p = *o;  // added to: a plain bf16 output is not WIDE
+            *o = u32x2{pack_bf16(bf16_lo(p.x) + v.x, bf16_hi(p.x) + v.y),
+                       pack_bf16(bf16_lo(p.y) + v.z, bf16_hi(p.y) + v.w)};
+          }
         } else {
-          u32x2 *o = reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.out) + t * a.ldo + n);
-          const u32x2 p = *o;  // added to: a plain bf16 output is not WIDE
-          *o = u32x2{pack_bf16(bf16_lo(p.x) + v.x, bf16_hi(p.x) + v.y),
-                     pack_bf16(bf16_lo(p.y) + v.z, bf16_hi(p.y) + v.w)};
+          *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out) + t * a.ldo + n) = w;
         }
-      } else {
-        const int64_t n = n0 + c * 8;
-        if (n < a.n) *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out) + t * a.ldo + n) = w;
       }
     }
   }
 }
 
+// Tile `id` of the order in which an XCD's 32 workgroups share rows of both operands in their
+// L2: groups 8 token tiles tall.
+__device__ __forceinline__ void tile_of(int id, int tiles_t, int tiles_n, int64_t &t0, int64_t &n0) {
+  const int per_group = kGroupT * tiles_n;
+  const int first_t = (id / per_group) * kGroupT;
+  const int gt = tiles_t - first_t < kGroupT ? tiles_t - first_t : kGroupT;
+  t0 = (int64_t)__builtin_amdgcn_readfirstlane(first_t + (id % per_group) % gt) * kTile;
+  n0 = (int64_t)__builtin_amdgcn_readfirstlane((id % per_group) / gt) * kTile;
+}
+
+__device__ __forceinline__ TileSource tile_source(const Int8Args &a, int64_t t0, int64_t n0) {
+  const int64_t rows_t = a.tokens - t0 < kTile ? a.tokens - t0 : kTile;
+  const int64_t rows_n = a.n - n0 < kTile ? a.n - n0 : kTile;
+  TileSource s;
+  s.a = __builtin_amdgcn_make_buffer_rsrc((void *)(a.a + t0 * a.k), 0, (int)(rows_t * a.k), 0x00020000);
+  s.b = __builtin_amdgcn_make_buffer_rsrc((void *)(a.w + n0 * a.k), 0, (int)(rows_n * a.k), 0x00020000);
+  return s;
+}
+
+// A workgroup stays for every `groups`-th tile of its XCD.  The stages of its tiles follow one
+// another in the ring without a gap: while a tile's last four stages are multiplied, the next
+// tile's first four are loaded, and they land while the outputs are written.
 template <bool WIDE>
 __global__ __launch_bounds__(kTileThreads, 1) void int8_tile_kernel(const Int8Args a, int tiles_t,
                                                                     int tiles_n) {
@@ -487,88 +537,92 @@ __global__ __launch_bounds__(kTileThreads, 1) void int8_tile_kernel(const Int8Ar
   __shared__ __attribute__((aligned(16))) uint8_t a1[kStageBytes], b1[kStageBytes];
   __shared__ __attribute__((aligned(16))) uint8_t a2[kStageBytes], b2[kStageBytes];
   __shared__ __attribute__((aligned(16))) uint8_t a3[kStageBytes], b3[kStageBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t rows[4][4096];
+  __shared__ __attribute__((aligned(16))) TileScales scales[2];
 
-  // each XCD takes a contiguous run of tiles, in groups 8 token tiles tall, so that its CUs
-  // share rows of both operands in their L2
-  int id = blockIdx.x;
-  {
-    const int n = tiles_t * tiles_n, x = id & 7, q = n >> 3, r = n & 7;
-    id = x * q + (x < r ? x : r) + (id >> 3);
-  }
-  const int per_group = kGroupT * tiles_n;
-  const int first_t = (id / per_group) * kGroupT;
-  const int gt = tiles_t - first_t < kGroupT ? tiles_t - first_t : kGroupT;
-  const int tile_t = __builtin_amdgcn_readfirstlane(first_t + (id % per_group) % gt);
-  const int tile_n = __builtin_amdgcn_readfirstlane((id % per_group) / gt);
-  const int64_t t0 = (int64_t)tile_t * kTile, n0 = (int64_t)tile_n * kTile;
+  // XCD x (workgroups are dealt round robin) has the tiles [first, last) of the order, its
+  // workgroups take them in turn
+  const int tiles = tiles_t * tiles_n, x = blockIdx.x & 7;
+  const int per = tiles >> 3, more = tiles & 7;
+  const int first = x * per + (x < more ? x : more), last = first + per + (x < more ? 1 : 0);
+  const int stride = ((int)gridDim.x - x + 7) >> 3;
+  int id = first + ((int)blockIdx.x >> 3);
+  if (id >= last) return;
 
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63;
   const int wt = wave >> 1, wn = wave & 1;
 
-  const int64_t rows_t = a.tokens - t0 < kTile ? a.tokens - t0 : kTile;
-  const int64_t rows_n = a.n - n0 < kTile ? a.n - n0 : kTile;
-  const __amdgpu_buffer_rsrc_t ra =
-      __builtin_amdgcn_make_buffer_rsrc((void *)(a.a + t0 * a.k), 0, (int)(rows_t * a.k), 0x00020000);
-  const __amdgpu_buffer_rsrc_t rb =
-      __builtin_amdgcn_make_buffer_rsrc((void *)(a.w + n0 * a.k), 0, (int)(rows_n * a.k), 0x00020000);
   TileLoad tl;
   {
     const int row = lane >> 2;
-    tl.g16 = ((lane & 3) ^ ((row >> 1) & 3)) * 16;
+    tl.g16 = ((lane & 3) ^ ((row >> 2) & 3)) * 16;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int x = wave * 64 + r * 16 + row;  // rows past the operand lie past its range
-      tl.a[r] = (uint32_t)x * (uint32_t)a.k + (uint32_t)tl.g16;
-      tl.b[r] = tl.a[r];
-    }
+    for (int r = 0; r < 4; ++r)  // rows past the operand lie past its range
+      tl.row[r] = (uint32_t)(wave * 64 + r * 16 + row) * (uint32_t)a.k + (uint32_t)tl.g16;
   }
   uint32_t oa[2], ob[2];
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) {
     const int r = lane & 31, g = 2 * ks + (lane >> 5);
-    const uint32_t o = (uint32_t)(r * kStageK + ((g ^ ((r >> 1) & 3)) << 4));
+    const uint32_t o = (uint32_t)(r * kStageK + ((g ^ ((r >> 2) & 3)) << 4));
     oa[ks] = o + (uint32_t)(wt * 128 * kStageK);
     ob[ks] = o + (uint32_t)(wn * 128 * kStageK);
   }
 
-  i32x16 acc[4][4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = i32x16{};
-
-  const int k = a.k, stages = (k + kStageK - 1) / kStageK;
-  dma_stage(ra, rb, tl, 0, k, a0, b0, wave);
-  dma_stage(ra, rb, tl, kStageK, k, a1, b1, wave);
-  dma_stage(ra, rb, tl, 2 * kStageK, k, a2, b2, wave);
-  dma_stage(ra, rb, tl, 3 * kStageK, k, a3, b3, wave);
+  const int k = a.k;
+  int64_t t0, n0, next_t0 = 0, next_n0 = 0;
+  tile_of(id, tiles_t, tiles_n, t0, n0);
+  TileSource src = tile_source(a, t0, n0);
+  dma_stage(src, tl, 0, k, a0, b0, wave);
+  dma_stage(src, tl, kStageK, k, a1, b1, wave);
+  dma_stage(src, tl, 2 * kStageK, k, a2, b2, wave);
+  dma_stage(src, tl, 3 * kStageK, k, a3, b3, wave);
   barrier_but_vmcnt<3 * kStageLoads>();
   TileFrags f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) read_block<0>(f, a0, b0, oa, ob, i);
-  int k4 = 4 * kStageK;
-  for (int s = 4; s <= stages; s += 4, k4 += 4 * kStageK) {
-    tile_stage(acc, f, a0, b0, a1, b1, ra, rb, tl, k4, k, oa, ob, wave);
-    tile_stage(acc, f, a1, b1, a2, b2, ra, rb, tl, k4 + kStageK, k, oa, ob, wave);
-    tile_stage(acc, f, a2, b2, a3, b3, ra, rb, tl, k4 + 2 * kStageK, k, oa, ob, wave);
-    tile_stage(acc, f, a3, b3, a0, b0, ra, rb, tl, k4 + 3 * kStageK, k, oa, ob, wave);
-  }
-  // one to three stages left, rounded up to two or four (a stage past k is zeros)
-  if ((stages & 3) != 0) {
-    tile_stage(acc, f, a0, b0, a1, b1, ra, rb, tl, k4, k, oa, ob, wave);
-    tile_stage(acc, f, a1, b1, a2, b2, ra, rb, tl, k4 + kStageK, k, oa, ob, wave);
-    if ((stages & 3) == 3) {
-      tile_stage(acc, f, a2, b2, a3, b3, ra, rb, tl, k4 + 2 * kStageK, k, oa, ob, wave);
-    }
-  }
-  barrier_but_vmcnt<0>();  // loads past the last stage still write LDS
 
-  // the wave's own 32 KB of LDS: two of the stage buffers
-  uint8_t *const lo = wave == 0 ? a0 : wave == 1 ? a1 : wave == 2 ? a2 : a3;
-  uint8_t *const hi = wave == 0 ? b0 : wave == 1 ? b1 : wave == 2 ? b2 : b3;
-  tile_store<WIDE>(acc, a, lo, hi, t0 + wt * 128, n0 + wn * 128, lane);
+  int turn = 0;
+  for (;;) {
+    i32x16 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = i32x16{};
+    // the other tile's are still being read by waves that have not passed this tile's first
+    // barrier
+    dma_scales(a, t0, n0, scales[turn], wave, lane);
+    // four stages a turn (the last ones past k are zeros); k4: what is loaded meanwhile
+    bool more_tiles = true;
+    for (int k4 = 4 * kStageK;; k4 += 4 * kStageK) {
+      const bool end = k4 >= k;
+      int at = k4;
+      if (end) {
+        at = 0;
+        id += stride;
+        more_tiles = id < last;
+        if (more_tiles) {
+          tile_of(id, tiles_t, tiles_n, next_t0, next_n0);
+          src = tile_source(a, next_t0, next_n0);
+        } else {
+          at = k;  // nothing more: zeros
+        }
+      }
+      tile_stage(acc, f, a0, b0, a1, b1, src, tl, at, k, oa, ob, wave);
+      tile_stage(acc, f, a1, b1, a2, b2, src, tl, at + kStageK, k, oa, ob, wave);
+      tile_stage(acc, f, a2, b2, a3, b3, src, tl, at + 2 * kStageK, k, oa, ob, wave);
+      tile_stage(acc, f, a3, b3, a0, b0, src, tl, at + 3 * kStageK, k, oa, ob, wave);
+      if (end) break;
+    }
+    tile_store<WIDE>(acc, a, scales[turn], rows[wave], t0, n0, wt, wn, lane);
+    turn ^= 1;
+    if (!more_tiles) break;
+    t0 = next_t0;
+    n0 = next_n0;
+  }
+  barrier_but_vmcnt<0>();  // loads past the last tile still write LDS
 }
 
 }  // namespace
@@ -646,7 +700,8 @@ hipError_t launch_int8(const Int8Args &a, hipStream_t s) {
     return hipGetLastError();
   }
   const int tiles_t = (int)((a.tokens + kTile - 1) / kTile), tiles_n = (int)((a.n + kTile - 1) / kTile);
-  const dim3 grid(tiles_t * tiles_n), block(kTileThreads);
+  const int tiles = tiles_t * tiles_n;
+  const dim3 grid(tiles < kTileGroups ? tiles : kTileGroups), block(kTileThreads);
   if (a.out_f32 || a.accumulate)
     hipLaunchKernelGGL(int8_tile_kernel<true>, grid, block, 0, s, a, tiles_t, tiles_n);
   else
