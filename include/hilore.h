@@ -586,8 +586,8 @@ hilore_status hilore_block_norm_bwd(const hilore_block_norm_bwd_desc *d, int cod
  * (quantize: 1 for hilore_int8_linear, 0 for hilore_int8_matmul; 0 bytes, and then NULL
  * is allowed, where none is needed), 16-byte aligned, contents on entry irrelevant;
  * calls sharing it must not overlap.
- * Limits: k % 16 == 0, n % 8 == 0, k <= 131072, n < 2^26, tokens < 2^31 (else
- * UNSUPPORTED); k = 0 writes bias or zeros.
+ * Limits: k % 16 == 0, n % 8 == 0, k <= 131072, n < 2^26, tokens < 2^31, tokens * n <=
+ * 2^40 (else UNSUPPORTED); k = 0 writes bias or zeros.
  */
 typedef struct hilore_int8_desc {
   const uint16_t *x;

@@ -120,11 +120,17 @@ hilore::SavedRows saved_rows(const hilore_unit_desc &u, bool scaled) {
 }
 
 // ----------------------------------------------------------- int8 products --
-hilore_status check_int8(const hilore_int8_desc &d, bool quantize) {
+hilore_status check_int8_sizes(const hilore_int8_desc &d) {
   if (d.tokens < 0 || d.k < 0 || d.n < 0) return HILORE_ERR_INVALID_ARG;
   if (d.k % 16 != 0 || d.n % 8 != 0 || d.k > hilore::kInt8MaxK || d.n >= (int64_t(1) << 26) ||
-      d.tokens >= (int64_t(1) << 31))
+      d.tokens >= (int64_t(1) << 31) || d.tokens * d.n > hilore::kInt8MaxOut)
     return HILORE_ERR_UNSUPPORTED;
+  return HILORE_OK;
+}
+
+hilore_status check_int8(const hilore_int8_desc &d, bool quantize) {
+  const hilore_status sizes = check_int8_sizes(d);
+  if (sizes != HILORE_OK) return sizes;
   if (d.tokens == 0 || d.n == 0) return HILORE_OK;
   if (!d.out || d.ldo < d.n) return HILORE_ERR_INVALID_ARG;
   if (d.ldo % 8 != 0) return HILORE_ERR_ALIGNMENT;
@@ -328,7 +334,7 @@ hilore_status hilore_block_norm_bwd(const hilore_block_norm_bwd_desc *d, int cod
 }
 
 size_t hilore_int8_workspace_bytes(const hilore_int8_desc *d, int quantize) {
-  if (!d || d->tokens <= 0 || d->n <= 0 || d->k < 0) return 0;
+  if (!d || d->tokens == 0 || d->n == 0 || check_int8_sizes(*d) != HILORE_OK) return 0;
   return int8_layout(*d, quantize != 0).bytes;
 }
 

@@ -382,6 +382,7 @@ struct Int8Args {
   int32_t *part;  // workspace
 };
 constexpr int64_t kInt8MaxK = 131072;  // 2^17 * 127^2 < 2^31
+constexpr int64_t kInt8MaxOut = int64_t(1) << 40;  // tokens * n: tiles are counted in 32 bits
 size_t int8_part_bytes(int64_t tokens, int64_t k, int64_t n);
 hipError_t launch_int8(const Int8Args &a, hipStream_t s);
 

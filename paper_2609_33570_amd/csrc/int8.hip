@@ -309,21 +309,31 @@ __global__ __launch_bounds__(256) void int8_join_kernel(const Int8Args a, int pa
   }
 }
 
-// ------------------------------------------------------------- large tiles --
-// 256 tokens x 256 channels per workgroup of 4 waves (2 x 2), each wave 128 x 128 =
-// 4 x 4 blocks of v_mfma_i32_32x32x32_i8, one wave a SIMD.  Both operands have k
-// contiguous, so they are copied to LDS as they are by the buffer unit (16-byte
-// LDS-DMA loads, no registers) in stages of 64 k: [256 rows][64 B] each, 16-byte
-// chunk g of row r at position g ^ (r / 4 % 4), which spreads the 16 rows that one
-// cycle of a fragment read takes over all banks.  Four stages are in flight.
-constexpr int kTile = 256, kStageK = 64, kTileThreads = 256;
-constexpr int kStageBytes = kTile * kStageK;  // of one operand (16 KB)
-constexpr int kStageLoads = 8;                // LDS-DMA instructions of a wave per stage
+// ------------------------------------------------------------------- tiles --
+// 64 B tokens x 64 B channels (B = 4: 256, B = 2: 128) per workgroup of 4 waves (2 x 2), each
+// wave B x B blocks of v_mfma_i32_32x32x32_i8, one wave a SIMD.  Both operands have k
+// contiguous, so they are copied to LDS as they are by the buffer unit (16-byte LDS-DMA loads,
+// no registers) in stages of 64 k: [64 B rows][64 bytes] each, 16-byte chunk g of row r at
+// position g ^ (r / 4 % 4), which spreads the 16 rows that one cycle of a fragment read takes
+// over all banks.  Four stages are in flight.
+// A large product is bound by the matrix units at the clock their power allows: 16384 x 3584 x 18944
+// takes 1166 us, 1.91 POP/s; the outputs' way through LDS (5 us a tile) is not covered by products.
+constexpr int kStageK = 64, kTileThreads = 256;
+constexpr int kTurnK = 4 * kStageK;  // a turn of the ring
 constexpr int kGroupT = 8;
-constexpr int kTileGroups = 256;              // one a CU
 
+template <int B>
+struct Tile {
+  static constexpr int kSide = 64 * B;
+  static constexpr int kStageBytes = kSide * kStageK;  // of one operand
+  static constexpr int kStageLoads = 2 * B;            // LDS-DMA instructions of a wave per stage
+  static constexpr int kRow = 32 * B;                  // bytes of a token that a wave writes at a time
+  static constexpr int kPerCu = B == 2 ? 2 : 1;        // workgroups, by their LDS
+};
+
+template <int B>
 struct TileLoad {
-  uint32_t row[4];  // byte offset of the lane's chunk in its row of each load, at k = 0
+  uint32_t row[B];  // byte offset of the lane's chunk in its row of each load, at k = 0
   int g16;          // its first k within a stage
 };
 
@@ -331,61 +341,55 @@ struct TileSource {  // the operands' rows of one tile
   __amdgpu_buffer_rsrc_t a, b;
 };
 
-// Stage k0 of both operands into `la`, `lb`: load r of wave w writes rows 64 w + 16 r ..
-// + 15, lane l the chunk at position l % 4 of row l / 4.  Chunks past k read as 0.
-__device__ __forceinline__ void dma_stage(const TileSource &src, const TileLoad &tl, int k0, int k,
-                                          uint8_t *la, uint8_t *lb, int wave) {
-  const uint32_t past = k0 + tl.g16 < k ? 0u : kOob;
+// Stage k0 of both operands into `la`, `lb`: load r of wave w writes rows 16 (B w + r) ..
+// + 15, lane l the chunk at position l % 4 of row l / 4.  Chunks past `end` read as 0.
+template <int B>
+__device__ __forceinline__ void dma_stage(const TileSource &src, const TileLoad<B> &tl, int k0,
+                                          int end, uint8_t *la, uint8_t *lb, int wave) {
+  const uint32_t past = k0 + tl.g16 < end ? 0u : kOob;
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int off = (int)((tl.row[r] + (uint32_t)k0) | past), to = (wave * 64 + r * 16) * kStageK;
+  for (int r = 0; r < B; ++r) {
+    const int off = (int)((tl.row[r] + (uint32_t)k0) | past), to = (wave * B + r) * 16 * kStageK;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(src.a, (lds_void *)(la + to), 16, off, 0, 0, 0);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(src.b, (lds_void *)(lb + to), 16, off, 0, 0, 0);
   }
 }
 
+template <int B>
 struct TileFrags {
-  i32x4 a[2][4], b[2][4];  // fragments of even and odd k-steps
+  i32x4 a[2][B], b[2][B];  // fragments of even and odd k-steps
 };
 
 // Fragments of k-step KS (32 k) of a stage: lane l takes chunk 2 KS + l / 32 of row l % 32
 // of each 32-row block; oa, ob: the lane's offset in block 0 at KS = 0 and at KS = 1.
-template <int KS>
-__device__ __forceinline__ void read_block(TileFrags &f, const uint8_t *la, const uint8_t *lb,
+template <int KS, int B>
+__device__ __forceinline__ void read_block(TileFrags<B> &f, const uint8_t *la, const uint8_t *lb,
                                            const uint32_t (&oa)[2], const uint32_t (&ob)[2],
                                            int i) {
   f.a[KS][i] = *reinterpret_cast<const i32x4 *>(la + oa[KS] + i * 32 * kStageK);
   f.b[KS][i] = *reinterpret_cast<const i32x4 *>(lb + ob[KS] + i * 32 * kStageK);
 }
 
-// The 16 products of k-step KS with the reads of the other k-step's fragments (from la, lb).
-template <int KS>
-__device__ __forceinline__ void mma16(i32x16 (&acc)[4][4], TileFrags &f, const uint8_t *la,
-                                      const uint8_t *lb, const uint32_t (&oa)[2],
-                                      const uint32_t (&ob)[2]) {
+// The products of k-step KS with the reads of the other k-step's fragments (from la, lb), a
+// read after each of the first 2 B MFMAs, so that they are there when the next region begins;
+// LOADS: an LDS-DMA load after each of the others (B = 2: after every read).
+template <int KS, bool LOADS, int B>
+__device__ __forceinline__ void mma_step(i32x16 (&acc)[B][B], TileFrags<B> &f, const uint8_t *la,
+                                         const uint8_t *lb, const uint32_t (&oa)[2],
+                                         const uint32_t (&ob)[2]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) read_block<KS ^ 1>(f, la, lb, oa, ob, i);
+  for (int i = 0; i < B; ++i) read_block<KS ^ 1>(f, la, lb, oa, ob, i);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < B; ++i) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < B; ++j)
       acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.b[KS][i], f.a[KS][j], acc[i][j], 0, 0, 0);
   }
-}
-
-// The other k-step's 8 fragment reads after the first 8 MFMAs, so that they are there when
-// the next region begins; the loads, if any, after the last 8.
-template <bool LOADS>
-__device__ __forceinline__ void schedule16() {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // 1 MFMA
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // 1 LDS read
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    if constexpr (LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // 1 LDS-DMA load
+  for (int i = 0; i < B * B; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                        // 1 MFMA
+    if (i < 2 * B) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);         // 1 LDS read
+    if (LOADS && (B == 2 || i >= 2 * B)) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
   }
   __builtin_amdgcn_sched_barrier(0);
 }
@@ -395,18 +399,17 @@ __device__ __forceinline__ void schedule16() {
 // they have landed for all waves and that nobody reads stage s from LDS any more; the second
 // k-step's products then cover the loads of stage s + 4 into its place and the first
 // fragment reads of stage s + 1.
-__device__ __forceinline__ void tile_stage(i32x16 (&acc)[4][4], TileFrags &f, uint8_t *cur_a,
+template <int B>
+__device__ __forceinline__ void tile_stage(i32x16 (&acc)[B][B], TileFrags<B> &f, uint8_t *cur_a,
                                            uint8_t *cur_b, const uint8_t *nxt_a,
                                            const uint8_t *nxt_b, const TileSource &src,
-                                           const TileLoad &tl, int k4, int k,
+                                           const TileLoad<B> &tl, int k4, int end,
                                            const uint32_t (&oa)[2], const uint32_t (&ob)[2],
                                            int wave) {
-  mma16<0>(acc, f, cur_a, cur_b, oa, ob);
-  schedule16<false>();
-  barrier_but_vmcnt<2 * kStageLoads>();
-  dma_stage(src, tl, k4, k, cur_a, cur_b, wave);
-  mma16<1>(acc, f, nxt_a, nxt_b, oa, ob);
-  schedule16<true>();
+  mma_step<0, false>(acc, f, cur_a, cur_b, oa, ob);
+  barrier_but_vmcnt<2 * Tile<B>::kStageLoads>();
+  dma_stage(src, tl, k4, end, cur_a, cur_b, wave);
+  mma_step<1, true>(acc, f, nxt_a, nxt_b, oa, ob);
 }
 
 // One accumulator value, where it is asked for: left to itself the compiler copies all 256 at
@@ -418,132 +421,161 @@ __device__ __forceinline__ int acc_value(int a) {
   return v;
 }
 
-// Scales and bias of one tile in LDS, copied there while the tile before is at work.
+// Scales and bias of one tile in LDS, copied there while the tile is at work.
+template <int B>
 struct TileScales {
-  float sa[kTile], sw[kTile];
-  uint16_t bias[kTile];
+  float sa[Tile<B>::kSide], sw[Tile<B>::kSide];
+  uint16_t bias[Tile<B>::kSide];
 };
 
-__device__ __forceinline__ void dma_scales(const Int8Args &a, int64_t t0, int64_t n0, TileScales &s,
-                                           int wave, int lane) {
-  const int64_t rows_t = a.tokens - t0 < kTile ? a.tokens - t0 : kTile;
-  const int64_t rows_n = a.n - n0 < kTile ? a.n - n0 : kTile;
+template <int B>
+__device__ __forceinline__ void dma_scales(const Int8Args &a, int64_t t0, int64_t n0,
+                                           TileScales<B> &s, int wave, int lane) {
+  constexpr int S = Tile<B>::kSide;
+  const int64_t rows_t = a.tokens - t0 < S ? a.tokens - t0 : S;
+  const int64_t rows_n = a.n - n0 < S ? a.n - n0 : S;
   const auto copy = [&](const void *from, int64_t bytes, void *to) {
     const __amdgpu_buffer_rsrc_t r =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(from), 0, (int)bytes, 0x00020000);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)((uint8_t *)to + wave * 256), 4,
                                              (wave * 64 + lane) * 4, 0, 0, 0);
   };
-  copy(a.a_scales + t0, rows_t * 4, s.sa);
-  if (a.w_scales) copy(a.w_scales + n0, rows_n * 4, s.sw);
-  if (a.bias && wave < 2) copy(a.bias + n0, rows_n * 2, s.bias);
+  if (wave < B) copy(a.a_scales + t0, rows_t * 4, s.sa);
+  if (a.w_scales && wave < B) copy(a.w_scales + n0, rows_n * 4, s.sw);
+  if (a.bias && wave < B / 2) copy(a.bias + n0, rows_n * 2, s.bias);
 }
 
-// A wave's 128 x 128 outputs.  Accumulator block (i, j): lane l holds token l % 32 of block j
+// What becomes of a tile's sums: a bf16 output; an fp32 one, or a bf16 one that is added to
+// (in fp32, one rounding); raw sums of a part of k in the workspace.
+enum Store : int { kStoreBf16, kStoreWide, kStorePart };
+
+// One piece of work: a tile, or the part of k from `begin` to `end` of one.
+struct TileWork {
+  int64_t t0, n0;
+  int part, begin, end;
+};
+
+// A wave's 32 B x 32 B outputs.  Accumulator block (i, j): lane l holds token l % 32 of block j
 // and, in register 4 q + e, channel 8 q + 4 (l / 32) + e of block i.  The values go through the
-// wave's 4 KB of LDS, 32 tokens of 128 B at a time with 16-byte chunk c of a token at
-// c ^ (token % 8), so that the output is written in whole lines.  WIDE: as fp32, a block of 32
-// channels at a time (fp32 outputs, and bf16 ones that are added to: one rounding); else as
-// bf16, two blocks.
-template <bool WIDE>
-__device__ __forceinline__ void tile_store(const i32x16 (&acc)[4][4], const Int8Args &a,
-                                           const TileScales &s, uint8_t *lds, int64_t t0,
-                                           int64_t n0, int wt, int wn, int lane) {
-  constexpr int kBlocks = WIDE ? 1 : 2;
+// wave's LDS, 32 tokens of kRow bytes at a time with their 16-byte chunks permuted so that 16
+// tokens cover all banks, so that the output is written in whole rows of kRow bytes.
+template <int MODE, int B>
+__device__ __forceinline__ void tile_store(const i32x16 (&acc)[B][B], const Int8Args &a,
+                                           const TileScales<B> &s, uint8_t *lds, const TileWork &w,
+                                           int wt, int wn, int lane) {
+  constexpr int kRow = Tile<B>::kRow, kChunks = kRow / 16, kWave = 32 * B;
+  constexpr int kChannels = kRow / (MODE == kStoreBf16 ? 2 : 4);
   asm volatile("s_nop 15\n\ts_nop 15");  // more than the 18 states from an MFMA to a read of its result
   asm volatile("" : "+v"(lane));  // else the addresses below are formed once and kept, 100 registers
   const int h = lane >> 5, tok = lane & 31;
-  const int c = lane & 7, sub = lane >> 3;
+  const int c = lane % kChunks, sub = lane / kChunks;
+  const auto at = [](int row, int chunk) {
+    return row * kRow + ((chunk ^ (row / (16 / kChunks) % kChunks)) << 4);
+  };
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float sa = s.sa[wt * 128 + j * 32 + tok];
+  for (int j = 0; j < B; ++j) {
+    const float sa = MODE == kStorePart ? 1.0f : s.sa[wt * kWave + j * 32 + tok];
 #pragma unroll
-    for (int i0 = 0; i0 < 4; i0 += kBlocks) {
+    for (int c0 = 0; c0 < kWave; c0 += kChannels) {
 #pragma unroll
-      for (int i = i0; i < i0 + kBlocks; ++i) {
+      for (int qq = 0; qq < kChannels / 8; ++qq) {
+        const int i = (c0 + qq * 8) / 32, q = (c0 + qq * 8) % 32 / 8;
+        i32x4 sum;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int at = wn * 128 + i * 32 + q * 8 + h * 4;
-          f32x4 v;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = (float)acc_value(acc[i][j][4 * q + e]) * sa;
-          if (a.w_scales) v *= *reinterpret_cast<const f32x4 *>(s.sw + at);
-          if (a.bias) {
-            const u32x2 b = *reinterpret_cast<const u32x2 *>(s.bias + at);
-            v += f32x4{bf16_lo(b.x), bf16_hi(b.x), bf16_lo(b.y), bf16_hi(b.y)};
-          }
-          uint8_t *row = lds + tok * 128;
-          if constexpr (WIDE) {
-            *reinterpret_cast<f32x4 *>(row + (((q * 2 + h) ^ (tok & 7)) << 4)) = v;
-          } else {
-            *reinterpret_cast<u32x2 *>(row + ((((i - i0) * 4 + q) ^ (tok & 7)) << 4) + h * 8) =
-                u32x2{pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)};
-          }
+        for (int e = 0; e < 4; ++e) sum[e] = acc_value(acc[i][j][4 * q + e]);
+        if constexpr (MODE == kStorePart) {
+          *reinterpret_cast<i32x4 *>(lds + at(tok, qq * 2 + h)) = sum;
+          continue;
+        }
+        const int ch = wn * kWave + i * 32 + q * 8 + h * 4;
+        f32x4 v = {(float)sum.x * sa, (float)sum.y * sa, (float)sum.z * sa, (float)sum.w * sa};
+        if (a.w_scales) v *= *reinterpret_cast<const f32x4 *>(s.sw + ch);
+        if (a.bias) {
+          const u32x2 b = *reinterpret_cast<const u32x2 *>(s.bias + ch);
+          v += f32x4{bf16_lo(b.x), bf16_hi(b.x), bf16_lo(b.y), bf16_hi(b.y)};
+        }
+        if constexpr (MODE == kStoreWide) {
+          *reinterpret_cast<f32x4 *>(lds + at(tok, qq * 2 + h)) = v;
+        } else {
+          *reinterpret_cast<u32x2 *>(lds + at(tok, qq) + h * 8) =
+              u32x2{pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)};
         }
       }
-      // a row of 8 chunks by 8 lanes, 8 rows at a time
 #pragma unroll
-      for (int it = 0; it < 4; ++it) {
-        const int r = it * 8 + sub;
-        const int64_t t = t0 + wt * 128 + j * 32 + r;
-        const int64_t n = n0 + wn * 128 + i0 * 32 + c * (WIDE ? 4 : 8);
-        const u32x4 w = *reinterpret_cast<const u32x4 *>(lds + r * 128 + ((c ^ (r & 7)) << 4));
+      for (int r = sub; r < 32 + sub; r += 64 / kChunks) {
+        const int64_t t = w.t0 + wt * kWave + j * 32 + r;
+        const int64_t n = w.n0 + wn * kWave + c0 + c * (kChannels / kChunks);
+        const u32x4 o4 = *reinterpret_cast<const u32x4 *>(lds + at(r, c));
         if (t >= a.tokens || n >= a.n) continue;
-        if constexpr (WIDE) {
-          f32x4 v = __builtin_bit_cast(f32x4, w);
+        if constexpr (MODE == kStorePart) {
+          *reinterpret_cast<u32x4 *>(a.part + ((int64_t)w.part * a.tokens + t) * a.n + n) = o4;
+        } else if constexpr (MODE == kStoreWide) {
+          f32x4 v = __builtin_bit_cast(f32x4, o4);
           if (a.out_f32) {
             f32x4 *o = reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + t * a.ldo + n);
             *o = a.accumulate ? *o + v : v;
           } else {
             u32x2 *o = reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.out) + t * a.ldo + n);
-            const u32x2 p = *o;  // added to: a plain bf16 output is not WIDE
+            const u32x2 p = *o;  // added to: a plain bf16 output is kStoreBf16
             *o = u32x2{pack_bf16(bf16_lo(p.x) + v.x, bf16_hi(p.x) + v.y),
                        pack_bf16(bf16_lo(p.y) + v.z, bf16_hi(p.y) + v.w)};
           }
         } else {
-          *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out) + t * a.ldo + n) = w;
+          *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out) + t * a.ldo + n) = o4;
         }
       }
     }
   }
 }
 
-// Tile `id` of the order in which an XCD's 32 workgroups share rows of both operands in their
-// L2: groups 8 token tiles tall.
-__device__ __forceinline__ void tile_of(int id, int tiles_t, int tiles_n, int64_t &t0, int64_t &n0) {
+// Piece `id` of the order in which an XCD's 32 workgroups share rows of both operands in their
+// L2: parts slowest, then groups 8 token tiles tall.
+template <int B>
+__device__ __forceinline__ TileWork work_of(const Int8Args &a, int id, int tiles_t, int tiles_n,
+                                            int parts) {
+  const int tiles = tiles_t * tiles_n;
+  TileWork w;
+  w.part = __builtin_amdgcn_readfirstlane(id / tiles);
+  id -= w.part * tiles;
   const int per_group = kGroupT * tiles_n;
   const int first_t = (id / per_group) * kGroupT;
   const int gt = tiles_t - first_t < kGroupT ? tiles_t - first_t : kGroupT;
-  t0 = (int64_t)__builtin_amdgcn_readfirstlane(first_t + (id % per_group) % gt) * kTile;
-  n0 = (int64_t)__builtin_amdgcn_readfirstlane((id % per_group) / gt) * kTile;
+  w.t0 = (int64_t)__builtin_amdgcn_readfirstlane(first_t + (id % per_group) % gt) * Tile<B>::kSide;
+  w.n0 = (int64_t)__builtin_amdgcn_readfirstlane((id % per_group) / gt) * Tile<B>::kSide;
+  const int turns = (a.k + kTurnK - 1) / kTurnK;  // <= 2^9, of at most 2^8 parts
+  w.begin = turns * w.part / parts * kTurnK;
+  const int end = turns * (w.part + 1) / parts * kTurnK;
+  w.end = end < a.k ? end : a.k;
+  return w;
 }
 
-__device__ __forceinline__ TileSource tile_source(const Int8Args &a, int64_t t0, int64_t n0) {
-  const int64_t rows_t = a.tokens - t0 < kTile ? a.tokens - t0 : kTile;
-  const int64_t rows_n = a.n - n0 < kTile ? a.n - n0 : kTile;
+template <int B>
+__device__ __forceinline__ TileSource tile_source(const Int8Args &a, const TileWork &w) {
+  constexpr int S = Tile<B>::kSide;
+  const int64_t rows_t = a.tokens - w.t0 < S ? a.tokens - w.t0 : S;
+  const int64_t rows_n = a.n - w.n0 < S ? a.n - w.n0 : S;
   TileSource s;
-  s.a = __builtin_amdgcn_make_buffer_rsrc((void *)(a.a + t0 * a.k), 0, (int)(rows_t * a.k), 0x00020000);
-  s.b = __builtin_amdgcn_make_buffer_rsrc((void *)(a.w + n0 * a.k), 0, (int)(rows_n * a.k), 0x00020000);
+  s.a = __builtin_amdgcn_make_buffer_rsrc((void *)(a.a + w.t0 * a.k), 0, (int)(rows_t * a.k), 0x00020000);
+  s.b = __builtin_amdgcn_make_buffer_rsrc((void *)(a.w + w.n0 * a.k), 0, (int)(rows_n * a.k), 0x00020000);
   return s;
 }
 
-// A workgroup stays for every `groups`-th tile of its XCD.  The stages of its tiles follow one
-// another in the ring without a gap: while a tile's last four stages are multiplied, the next
-// tile's first four are loaded, and they land while the outputs are written.
-template <bool WIDE>
-__global__ __launch_bounds__(kTileThreads, 1) void int8_tile_kernel(const Int8Args a, int tiles_t,
-                                                                    int tiles_n) {
-  __shared__ __attribute__((aligned(16))) uint8_t a0[kStageBytes], b0[kStageBytes];
-  __shared__ __attribute__((aligned(16))) uint8_t a1[kStageBytes], b1[kStageBytes];
-  __shared__ __attribute__((aligned(16))) uint8_t a2[kStageBytes], b2[kStageBytes];
-  __shared__ __attribute__((aligned(16))) uint8_t a3[kStageBytes], b3[kStageBytes];
-  __shared__ __attribute__((aligned(16))) uint8_t rows[4][4096];
-  __shared__ __attribute__((aligned(16))) TileScales scales[2];
+// A workgroup stays for every `groups`-th piece of its XCD.  Their stages follow one another in
+// the ring without a gap: while a piece's last four are multiplied, the next one's first four
+// are loaded, and they land while the outputs are written.
+template <int B, int MODE>
+__global__ __launch_bounds__(kTileThreads, Tile<B>::kPerCu) void int8_tile_kernel(const Int8Args a, int tiles_t,
+                                                                    int tiles_n, int parts) {
+  constexpr int kBytes = Tile<B>::kStageBytes;
+  __shared__ __attribute__((aligned(16))) uint8_t a0[kBytes], b0[kBytes], a1[kBytes], b1[kBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t a2[kBytes], b2[kBytes], a3[kBytes], b3[kBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t rows[4][32 * Tile<B>::kRow];
+  __shared__ __attribute__((aligned(16))) TileScales<B> scales[2];
 
-  // XCD x (workgroups are dealt round robin) has the tiles [first, last) of the order, its
+  // XCD x (workgroups are dealt round robin) has the pieces [first, last) of the order, its
   // workgroups take them in turn
-  const int tiles = tiles_t * tiles_n, x = blockIdx.x & 7;
-  const int per = tiles >> 3, more = tiles & 7;
+  const int pieces = tiles_t * tiles_n * parts, x = blockIdx.x & 7;
+  const int per = pieces >> 3, more = pieces & 7;
   const int first = x * per + (x < more ? x : more), last = first + per + (x < more ? 1 : 0);
   const int stride = ((int)gridDim.x - x + 7) >> 3;
   int id = first + ((int)blockIdx.x >> 3);
@@ -554,75 +586,73 @@ __global__ __launch_bounds__(kTileThreads, 1) void int8_tile_kernel(const Int8Ar
   const int lane = tid & 63;
   const int wt = wave >> 1, wn = wave & 1;
 
-  TileLoad tl;
+  TileLoad<B> tl;
   {
     const int row = lane >> 2;
     tl.g16 = ((lane & 3) ^ ((row >> 2) & 3)) * 16;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)  // rows past the operand lie past its range
-      tl.row[r] = (uint32_t)(wave * 64 + r * 16 + row) * (uint32_t)a.k + (uint32_t)tl.g16;
+    for (int r = 0; r < B; ++r)  // rows past the operand lie past its range
+      tl.row[r] = (uint32_t)((wave * B + r) * 16 + row) * (uint32_t)a.k + (uint32_t)tl.g16;
   }
   uint32_t oa[2], ob[2];
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) {
     const int r = lane & 31, g = 2 * ks + (lane >> 5);
     const uint32_t o = (uint32_t)(r * kStageK + ((g ^ ((r >> 2) & 3)) << 4));
-    oa[ks] = o + (uint32_t)(wt * 128 * kStageK);
-    ob[ks] = o + (uint32_t)(wn * 128 * kStageK);
+    oa[ks] = o + (uint32_t)(wt * 32 * B * kStageK);
+    ob[ks] = o + (uint32_t)(wn * 32 * B * kStageK);
   }
 
-  const int k = a.k;
-  int64_t t0, n0, next_t0 = 0, next_n0 = 0;
-  tile_of(id, tiles_t, tiles_n, t0, n0);
-  TileSource src = tile_source(a, t0, n0);
-  dma_stage(src, tl, 0, k, a0, b0, wave);
-  dma_stage(src, tl, kStageK, k, a1, b1, wave);
-  dma_stage(src, tl, 2 * kStageK, k, a2, b2, wave);
-  dma_stage(src, tl, 3 * kStageK, k, a3, b3, wave);
-  barrier_but_vmcnt<3 * kStageLoads>();
-  TileFrags f;
+  TileWork w = work_of<B>(a, id, tiles_t, tiles_n, parts), next = w;
+  TileSource src = tile_source<B>(a, w);
+  dma_stage(src, tl, w.begin, w.end, a0, b0, wave);
+  dma_stage(src, tl, w.begin + kStageK, w.end, a1, b1, wave);
+  dma_stage(src, tl, w.begin + 2 * kStageK, w.end, a2, b2, wave);
+  dma_stage(src, tl, w.begin + 3 * kStageK, w.end, a3, b3, wave);
+  barrier_but_vmcnt<3 * Tile<B>::kStageLoads>();
+  TileFrags<B> f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) read_block<0>(f, a0, b0, oa, ob, i);
+  for (int i = 0; i < B; ++i) read_block<0>(f, a0, b0, oa, ob, i);
 
   int turn = 0;
   for (;;) {
-    i32x16 acc[4][4];
+    i32x16 acc[B][B];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < B; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = i32x16{};
-    // the other tile's are still being read by waves that have not passed this tile's first
+      for (int j = 0; j < B; ++j) acc[i][j] = i32x16{};
+    // the other ones are still being read by waves that have not passed this piece's first
     // barrier
-    dma_scales(a, t0, n0, scales[turn], wave, lane);
-    // four stages a turn (the last ones past k are zeros); k4: what is loaded meanwhile
-    bool more_tiles = true;
-    for (int k4 = 4 * kStageK;; k4 += 4 * kStageK) {
-      const bool end = k4 >= k;
-      int at = k4;
-      if (end) {
-        at = 0;
+    if constexpr (MODE != kStorePart) dma_scales(a, w.t0, w.n0, scales[turn], wave, lane);
+    // a turn of four stages (the last ones past the end are zeros); `at`: what is loaded meanwhile
+    bool more_work = true;
+    for (int k = w.begin + kTurnK;; k += kTurnK) {
+      const bool done = k >= w.end;
+      int at = k;
+      if (done) {
         id += stride;
-        more_tiles = id < last;
-        if (more_tiles) {
-          tile_of(id, tiles_t, tiles_n, next_t0, next_n0);
-          src = tile_source(a, next_t0, next_n0);
+        more_work = id < last;
+        if (more_work) {
+          next = work_of<B>(a, id, tiles_t, tiles_n, parts);
+          src = tile_source<B>(a, next);
+          at = next.begin;
         } else {
-          at = k;  // nothing more: zeros
+          at = next.end = 0;  // nothing more: zeros
         }
       }
-      tile_stage(acc, f, a0, b0, a1, b1, src, tl, at, k, oa, ob, wave);
-      tile_stage(acc, f, a1, b1, a2, b2, src, tl, at + kStageK, k, oa, ob, wave);
-      tile_stage(acc, f, a2, b2, a3, b3, src, tl, at + 2 * kStageK, k, oa, ob, wave);
-      tile_stage(acc, f, a3, b3, a0, b0, src, tl, at + 3 * kStageK, k, oa, ob, wave);
-      if (end) break;
+      const int end = next.end;
+      tile_stage(acc, f, a0, b0, a1, b1, src, tl, at, end, oa, ob, wave);
+      tile_stage(acc, f, a1, b1, a2, b2, src, tl, at + kStageK, end, oa, ob, wave);
+      tile_stage(acc, f, a2, b2, a3, b3, src, tl, at + 2 * kStageK, end, oa, ob, wave);
+      tile_stage(acc, f, a3, b3, a0, b0, src, tl, at + 3 * kStageK, end, oa, ob, wave);
+      if (done) break;
     }
-    tile_store<WIDE>(acc, a, scales[turn], rows[wave], t0, n0, wt, wn, lane);
+    tile_store<MODE>(acc, a, scales[turn], rows[wave], w, wt, wn, lane);
     turn ^= 1;
-    if (!more_tiles) break;
-    t0 = next_t0;
-    n0 = next_n0;
+    if (!more_work) break;
+    w = next;
   }
-  barrier_but_vmcnt<0>();  // loads past the last tile still write LDS
+  barrier_but_vmcnt<0>();  // loads past the last piece still write LDS
 }
 
 }  // namespace
@@ -659,6 +689,12 @@ struct FewPlan {
   int channels, parts;  // channels of a workgroup
 };
 
+// 33 to 64 tokens times large weights go as tiles: 64 x 3584 x 18944 takes 25.5 us as tiles and 32.2
+// here, x 18944 x 3584 23.2 and 25.5, but x 3584 x 4608 13.9 and 11.7, x 896 x 128 7.3 and 5.5.
+bool runs_few(int64_t tokens, int64_t k, int64_t n) {
+  return tokens <= 32 || (tokens <= kFewTokens && k * n <= (int64_t)1 << 25);
+}
+
 FewPlan few_plan(int64_t tokens, int64_t k, int64_t n) {
   FewPlan p{};
   p.channels = tokens > 32 ? 64 : tokens > 16 || n > 16 * 256 ? 32 : 16;
@@ -669,29 +705,83 @@ FewPlan few_plan(int64_t tokens, int64_t k, int64_t n) {
   return p;
 }
 
+void launch_join(const Int8Args &a, int parts, hipStream_t s) {
+  const int64_t groups = (a.tokens * (a.n / 4) + 255) / 256;
+  hipLaunchKernelGGL(int8_join_kernel, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0, s,
+                     a, parts);
+}
+
 template <int TB, int NB, int G, int WAVES>
 void launch_few(const Int8Args &a, const FewPlan &p, hipStream_t s) {
   const int64_t tiles = (a.n + 16 * NB - 1) / (16 * NB);
   hipLaunchKernelGGL((int8_few_kernel<TB, NB, G, WAVES>), dim3((unsigned)(tiles * p.parts)),
                      dim3(WAVES * 64), 0, s, a, p.parts);
+  if (p.parts > 1) launch_join(a, p.parts, s);
+}
+
+// How a product runs that the few-token kernel does not take: in tiles of 256 x 256 or 128 x 128,
+// of all of k or of one of several parts of it.  The larger tile reads half as much per product
+// and wins where there are tiles for all CUs; the smaller one, parts of k, or both, where there
+// are not: 700 x 3584 x 3584 takes 18.4 us in small tiles and 44.0 in large ones,
+// 3000 x 3584 x 3584 54.7 and 50.8; 128 x 18944 x 3584 118 us whole and 28 in nine parts.  The plan
+// with the least estimated time is taken.  The estimate, in us, was fitted to both sides and 1, 2
+// and 4 parts at 39 shapes of 65 to 16384 tokens, of which it takes one within 5 % of the fastest.
+struct TilePlan {
+  int side, parts;
+};
+
+constexpr int kMaxParts = 32;
+
+TilePlan tile_plan(int64_t tokens, int64_t k, int64_t n) {
+  const int64_t turns = (k + kTurnK - 1) / kTurnK;
+  const double far = k * n > (int64_t)1 << 25 ? 1.4 : 1.0;  // weights from beyond the caches
+  TilePlan best{256, 1};
+  double least = 0.0;
+  for (const int side : {256, 128}) {
+    const double stage = (side == 256 ? 0.55 : 0.22) * far, ends = side == 256 ? 5.0 : 2.0;
+    const int64_t tiles = ((tokens + side - 1) / side) * ((n + side - 1) / side);
+    for (int parts = 1; parts == 1 || (parts <= turns && parts <= kMaxParts); ++parts) {
+      const int64_t rounds = (tiles * parts + 255) / 256;
+      double us = ends + (double)rounds * ((double)((turns + parts - 1) / parts) * 4 * stage + ends);
+      if (parts > 1) us += 3.0 + parts * (0.5 + (double)tokens * (double)n * 8 / 6e6);
+      if (least == 0.0 || us < least) {
+        least = us;
+        best = TilePlan{side, parts};
+      }
+      if (rounds > 4) break;  // work enough for every CU
+    }
+  }
+  return best;
+}
+
+template <int B>
+void launch_tiles(const Int8Args &a, const TilePlan &p, hipStream_t s) {
+  constexpr int S = Tile<B>::kSide;
+  const int tiles_t = (int)((a.tokens + S - 1) / S), tiles_n = (int)((a.n + S - 1) / S);
+  const int64_t pieces = (int64_t)tiles_t * tiles_n * p.parts;
+  constexpr int64_t kResident = 256 * Tile<B>::kPerCu;
+  const dim3 grid((unsigned)(pieces < kResident ? pieces : kResident)), block(kTileThreads);
   if (p.parts > 1) {
-    const int64_t groups = (a.tokens * (a.n / 4) + 255) / 256;
-    hipLaunchKernelGGL(int8_join_kernel, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0,
-                       s, a, p.parts);
+    hipLaunchKernelGGL((int8_tile_kernel<B, kStorePart>), grid, block, 0, s, a, tiles_t, tiles_n, p.parts);
+    launch_join(a, p.parts, s);
+  } else if (a.out_f32 || a.accumulate) {
+    hipLaunchKernelGGL((int8_tile_kernel<B, kStoreWide>), grid, block, 0, s, a, tiles_t, tiles_n, 1);
+  } else {
+    hipLaunchKernelGGL((int8_tile_kernel<B, kStoreBf16>), grid, block, 0, s, a, tiles_t, tiles_n, 1);
   }
 }
 
 }  // namespace
 
 size_t int8_part_bytes(int64_t tokens, int64_t k, int64_t n) {
-  if (tokens > kFewTokens || tokens <= 0 || n <= 0) return 0;
-  const FewPlan p = few_plan(tokens, k, n);
-  return p.parts > 1 ? (size_t)p.parts * (size_t)tokens * (size_t)n * sizeof(int32_t) : 0;
+  if (tokens <= 0 || n <= 0) return 0;
+  const int parts = runs_few(tokens, k, n) ? few_plan(tokens, k, n).parts : tile_plan(tokens, k, n).parts;
+  return parts > 1 ? (size_t)parts * (size_t)tokens * (size_t)n * sizeof(int32_t) : 0;
 }
 
 hipError_t launch_int8(const Int8Args &a, hipStream_t s) {
   if (a.tokens == 0 || a.n == 0) return hipSuccess;
-  if (a.tokens <= kFewTokens) {
+  if (runs_few(a.tokens, a.k, a.n)) {
     const FewPlan p = few_plan(a.tokens, a.k, a.n);
     if (a.tokens <= 16 && p.channels == 16) launch_few<1, 1, 2, 8>(a, p, s);
     else if (a.tokens <= 16) launch_few<1, 2, 1, 4>(a, p, s);
@@ -699,13 +789,9 @@ hipError_t launch_int8(const Int8Args &a, hipStream_t s) {
     else launch_few<4, 4, 1, 4>(a, p, s);
     return hipGetLastError();
   }
-  const int tiles_t = (int)((a.tokens + kTile - 1) / kTile), tiles_n = (int)((a.n + kTile - 1) / kTile);
-  const int tiles = tiles_t * tiles_n;
-  const dim3 grid(tiles < kTileGroups ? tiles : kTileGroups), block(kTileThreads);
-  if (a.out_f32 || a.accumulate)
-    hipLaunchKernelGGL(int8_tile_kernel<true>, grid, block, 0, s, a, tiles_t, tiles_n);
-  else
-    hipLaunchKernelGGL(int8_tile_kernel<false>, grid, block, 0, s, a, tiles_t, tiles_n);
+  const TilePlan p = tile_plan(a.tokens, a.k, a.n);
+  if (p.side == 256) launch_tiles<4>(a, p, s);
+  else launch_tiles<2>(a, p, s);
   return hipGetLastError();
 }
 

@@ -192,3 +192,11 @@ def test_binding_refuses():
         E.adamw_tensor(grad=f, m=c, v=c, p=f, m_scales=torch.zeros(2), v_scales=torch.zeros(1))
     with pytest.raises(ValueError, match="2 elements"):
         E.hilore_grad_norm(E.adamw_tensors([]), 1.0, torch.zeros(3))
+
+
+def test_int8_output_size(lib):  # noqa: F811
+    """More outputs than any memory holds: refused, and no workspace asked for."""
+    for quantize in (True, False):
+        assert product(lib, quantize, tokens=1 << 30, n=2048, ldo=2048) == UNSUP
+        d = make(E.hilore_int8_desc, dict(tokens=1 << 30, n=2048, k=64), {})
+        assert lib.hilore_int8_workspace_bytes(ctypes.byref(d), int(quantize)) == 0
