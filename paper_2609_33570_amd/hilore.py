@@ -182,7 +182,8 @@ def _p(t) -> Optional[int]:
     elements, so both are refused here."""
     if t is None:
         return None
-    _device(t)
+    if not t.is_cuda:
+        _device(t)
     if not t.is_contiguous():
         raise ValueError(f"libhilore takes dense tensors, got strides {tuple(t.stride())}")
     return t.data_ptr()
@@ -511,12 +512,16 @@ def _keeping(desc, *tensors):
     return desc
 
 
+_DTYPE_NAMES = {}  # torch.dtype -> its name, kept: a trainer describes thousands of tensors
+
+
 def _typed(t, name: str, *dtypes: str):
     """t, refused unless its dtype is one of `dtypes` (None passes)."""
     if t is not None:
-        import torch
-
-        if all(t.dtype is not getattr(torch, d) for d in dtypes):
+        got = _DTYPE_NAMES.get(t.dtype)
+        if got is None:
+            got = _DTYPE_NAMES[t.dtype] = str(t.dtype).split(".")[-1]
+        if got not in dtypes:
             raise TypeError(f"{name} must be {' or '.join(dtypes)}, got {t.dtype}")
     return t
 
@@ -692,16 +697,14 @@ def adamw_tensor(grad, m, v, p=None, p16=None, m_scales=None, v_scales=None, lr:
     n = int(grad.numel())
     eight = m_scales is not None or v_scales is not None
     state = ("float8_e4m3fn", "uint8") if eight else ("float32",)
-    _typed(p, "p", "float32"), _typed(p16, "p16", "bfloat16")
     _typed(grad, "grad", "float32", "bfloat16")
-    _typed(m, "m", *state), _typed(v, "v", *state)
-    _typed(m_scales, "m_scales", "float32"), _typed(v_scales, "v_scales", "float32")
-    for t, name in ((p, "p"), (p16, "p16"), (m, "m"), (v, "v")):
-        if t is not None and t.numel() != n:
+    for t, name, types in ((p, "p", ("float32",)), (p16, "p16", ("bfloat16",)), (m, "m", state), (v, "v", state)):
+        if t is not None and _typed(t, name, *types).numel() != n:
             raise ValueError(f"{name} has {t.numel()} elements, the gradient {n}")
-    for t, name in ((m_scales, "m_scales"), (v_scales, "v_scales")):
-        if t is not None and t.numel() != -(-n // ADAMW_BLOCK):
-            raise ValueError(f"{name} needs {-(-n // ADAMW_BLOCK)} elements, got {t.numel()}")
+    if eight:
+        for t, name in ((m_scales, "m_scales"), (v_scales, "v_scales")):
+            if t is not None and _typed(t, name, "float32").numel() != -(-n // ADAMW_BLOCK):
+                raise ValueError(f"{name} needs {-(-n // ADAMW_BLOCK)} elements, got {t.numel()}")
     desc = hilore_adamw_tensor(_p(p), _p(p16), _p(grad), _p(m), _p(v), _p(m_scales), _p(v_scales), n,
                                float(lr), float(weight_decay), 1 if grad.element_size() == 2 else 0)
     return _keeping(desc, p, p16, grad, m, v, m_scales, v_scales)
