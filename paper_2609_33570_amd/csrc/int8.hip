@@ -317,10 +317,10 @@ __global__ __launch_bounds__(256) void int8_join_kernel(const Int8Args a, int pa
 // position g ^ (r / 4 % 4), which spreads the 16 rows that one cycle of a fragment read takes
 // over all banks.  Four stages are in flight.
 // A large product is bound by the matrix units at the clock their power allows: 16384 x 3584 x 18944
-// takes 1166 us, 1.91 POP/s; the outputs' way through LDS (5 us a tile) is not covered by products.
+// takes 1080 us, 2.06 POP/s; the outputs' way through LDS (5 us a tile) is not covered by products.
 constexpr int kStageK = 64, kTileThreads = 256;
 constexpr int kTurnK = 4 * kStageK;  // a turn of the ring
-constexpr int kGroupT = 8;
+constexpr int kGroupT = 16, kBlockT = 8, kBlockN = 4;  // tiles
 
 template <int B>
 struct Tile {
@@ -528,8 +528,10 @@ __device__ __forceinline__ void tile_store(const i32x16 (&acc)[B][B], const Int8
   }
 }
 
-// Piece `id` of the order in which an XCD's 32 workgroups share rows of both operands in their
-// L2: parts slowest, then groups 8 token tiles tall.
+// Piece `id` of the order of work: parts slowest, then groups 16 token tiles tall, in them blocks
+// of 8 x 4 tiles.  An XCD's workgroups have a block and share its rows in their L2, and the blocks
+// at work at a time make up 16 x 16 tiles, whose rows come from memory once for all XCDs (with
+// rows of tiles to each XCD of their own 16384 x 3584 x 18944 takes 1166 us, so 1080).
 template <int B>
 __device__ __forceinline__ TileWork work_of(const Int8Args &a, int id, int tiles_t, int tiles_n,
                                             int parts) {
@@ -537,11 +539,18 @@ __device__ __forceinline__ TileWork work_of(const Int8Args &a, int id, int tiles
   TileWork w;
   w.part = __builtin_amdgcn_readfirstlane(id / tiles);
   id -= w.part * tiles;
-  const int per_group = kGroupT * tiles_n;
-  const int first_t = (id / per_group) * kGroupT;
-  const int gt = tiles_t - first_t < kGroupT ? tiles_t - first_t : kGroupT;
-  w.t0 = (int64_t)__builtin_amdgcn_readfirstlane(first_t + (id % per_group) % gt) * Tile<B>::kSide;
-  w.n0 = (int64_t)__builtin_amdgcn_readfirstlane((id % per_group) / gt) * Tile<B>::kSide;
+  const int group = id / (kGroupT * tiles_n), t_first = group * kGroupT;
+  const int gt = tiles_t - t_first < kGroupT ? tiles_t - t_first : kGroupT;
+  id -= t_first * tiles_n;
+  const int column = id / (gt * kBlockN), n_first = column * kBlockN;
+  const int gn = tiles_n - n_first < kBlockN ? tiles_n - n_first : kBlockN;
+  id -= n_first * gt;
+  const int block = id / (kBlockT * gn);
+  const int bt = gt - block * kBlockT < kBlockT ? gt - block * kBlockT : kBlockT;
+  id -= block * kBlockT * gn;
+  const int t = t_first + block * kBlockT + id % bt, n = n_first + id / bt;
+  w.t0 = (int64_t)__builtin_amdgcn_readfirstlane(t) * Tile<B>::kSide;
+  w.n0 = (int64_t)__builtin_amdgcn_readfirstlane(n) * Tile<B>::kSide;
   const int turns = (a.k + kTurnK - 1) / kTurnK;  // <= 2^9, of at most 2^8 parts
   w.begin = turns * w.part / parts * kTurnK;
   const int end = turns * (w.part + 1) / parts * kTurnK;
@@ -560,8 +569,8 @@ __device__ __forceinline__ TileSource tile_source(const Int8Args &a, const TileW
   return s;
 }
 
-// A workgroup stays for every `groups`-th piece of its XCD.  Their stages follow one another in
-// the ring without a gap: while a piece's last four are multiplied, the next one's first four
+// A workgroup stays for its pieces of all rounds.  Their stages follow one another in the ring
+// without a gap: while a piece's last four are multiplied, the next one's first four
 // are loaded, and they land while the outputs are written.
 template <int B, int MODE>
 __global__ __launch_bounds__(kTileThreads, Tile<B>::kPerCu) void int8_tile_kernel(const Int8Args a, int tiles_t,
@@ -572,14 +581,15 @@ __global__ __launch_bounds__(kTileThreads, Tile<B>::kPerCu) void int8_tile_kerne
   __shared__ __attribute__((aligned(16))) uint8_t rows[4][32 * Tile<B>::kRow];
   __shared__ __attribute__((aligned(16))) TileScales<B> scales[2];
 
-  // XCD x (workgroups are dealt round robin) has the pieces [first, last) of the order, its
-  // workgroups take them in turn
-  const int pieces = tiles_t * tiles_n * parts, x = blockIdx.x & 7;
-  const int per = pieces >> 3, more = pieces & 7;
-  const int first = x * per + (x < more ? x : more), last = first + per + (x < more ? 1 : 0);
-  const int stride = ((int)gridDim.x - x + 7) >> 3;
-  int id = first + ((int)blockIdx.x >> 3);
-  if (id >= last) return;
+  // every round of the grid takes the next gridDim.x pieces, XCD x (workgroups are dealt round
+  // robin) an eighth of them; -1: no more
+  const int pieces = tiles_t * tiles_n * parts, x = blockIdx.x & 7, slot = blockIdx.x >> 3;
+  const auto piece = [&](int begin) {
+    const int count = pieces - begin < (int)gridDim.x ? pieces - begin : (int)gridDim.x;
+    const int per = count >> 3, more = count & 7;
+    return slot < per + (x < more ? 1 : 0) ? begin + x * per + (x < more ? x : more) + slot : -1;
+  };
+  int begin = 0, id = piece(0);  // the grid is at most the pieces: every workgroup has one
 
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -630,8 +640,9 @@ __global__ __launch_bounds__(kTileThreads, Tile<B>::kPerCu) void int8_tile_kerne
       const bool done = k >= w.end;
       int at = k;
       if (done) {
-        id += stride;
-        more_work = id < last;
+        begin += (int)gridDim.x;
+        id = begin < pieces ? piece(begin) : -1;
+        more_work = id >= 0;
         if (more_work) {
           next = work_of<B>(a, id, tiles_t, tiles_n, parts);
           src = tile_source<B>(a, next);
