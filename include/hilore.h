@@ -680,8 +680,9 @@ hilore_status hilore_grad_norm(const hilore_adamw_tensor *tensors, int n_tensors
  * Salt 0: low half for m, high half for r, as the 16 bits below the code; salt
  * 0x3C6EF372: low half as the 16 bits below a bf16 parameter.  The same inputs and seed
  * give the same bits in every call.
- * All tensors may differ in every field; all are done by ceil(n_tensors / 44) launches.
- * Limits: n < 2^32 for a tensor (else UNSUPPORTED).  Errors: betas outside [0, 1), eps not
+ * All tensors may differ in every field; a launch takes 67 to 100 of them (fewer pointers
+ * that any of them has, more tensors).
+ * Limits: n < 2^32 for a tensor, addresses below 2^48 (else UNSUPPORTED).  Errors: betas outside [0, 1), eps not
  * a positive normal float, step < 1, null pointers, negative sizes, lr or weight_decay not
  * finite, one of m_scales and v_scales alone -> INVALID_ARG.
  */

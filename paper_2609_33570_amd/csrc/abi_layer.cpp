@@ -211,6 +211,11 @@ constexpr int64_t kMaxElements = int64_t(1) << 40;
 // A launch's work-items are counted in 32 bits; 2^23 workgroups of 256 are half of that.
 constexpr int64_t kMaxChunks = int64_t(1) << 23;
 
+// Pointers travel to the kernels as 48 bits.
+bool fits48(const void *p) { return (reinterpret_cast<uintptr_t>(p) >> 48) == 0; }
+uint32_t low32(const void *p) { return (uint32_t)reinterpret_cast<uintptr_t>(p); }
+uint32_t upper16(const void *p) { return (uint32_t)((uint64_t)reinterpret_cast<uintptr_t>(p) >> 32); }
+
 hilore_status check_gradients(const hilore_adamw_tensor *t, int n) {
   if (n < 0) return HILORE_ERR_INVALID_ARG;
   if (n == 0) return HILORE_OK;
@@ -222,6 +227,7 @@ hilore_status check_gradients(const hilore_adamw_tensor *t, int n) {
     if (t[i].n == 0) continue;
     if (!t[i].grad) return HILORE_ERR_INVALID_ARG;
     if (!aligned16(t[i].grad)) return HILORE_ERR_ALIGNMENT;
+    if (!fits48(t[i].grad)) return HILORE_ERR_UNSUPPORTED;
     total += t[i].n;
     if (total > kMaxElements) return HILORE_ERR_UNSUPPORTED;
   }
@@ -237,6 +243,9 @@ hilore_status check_states(const hilore_adamw_tensor *t, int n) {
     const void *ptrs[] = {t[i].p, t[i].p16, t[i].m, t[i].v};
     if (!all_aligned16(ptrs) || !aligned4(t[i].m_scales) || !aligned4(t[i].v_scales))
       return HILORE_ERR_ALIGNMENT;
+    for (const void *p : {(const void *)t[i].p, (const void *)t[i].p16, (const void *)t[i].m, (const void *)t[i].v,
+                          (const void *)t[i].m_scales, (const void *)t[i].v_scales})
+      if (!fits48(p)) return HILORE_ERR_UNSUPPORTED;
   }
   return HILORE_OK;
 }
@@ -246,12 +255,18 @@ int64_t norm_chunks(const hilore_adamw_tensor &t) {
   return (t.n + elems - 1) / elems;
 }
 
-// Empties a launch's batch of tensors.
-template <typename Batch>
-void clear(Batch &b, int &count) {
+void clear(hilore::NormBatch &b, int &count) {
   count = 0;
   b.chunks = 0;
   for (uint32_t &x : b.begin) x = ~0u;
+  for (uint32_t &x : b.upper) x = 0;
+}
+
+void clear(hilore::AdamwBatch &b, int &count) {
+  count = 0;
+  b.chunks = 0;
+  for (uint32_t &x : b.w) x = 0;
+  for (int i = 0; i < b.cap; ++i) b.w[i] = ~0u;
 }
 
 }  // namespace
@@ -409,9 +424,9 @@ hilore_status hilore_grad_norm(const hilore_adamw_tensor *tensors, int n_tensors
       const hilore_status fs = flush();
       if (fs != HILORE_OK) return fs;
     }
-    b.t[count].grad = tensors[i].grad;
-    b.t[count].n = (uint32_t)tensors[i].n;
-    b.t[count].grad16 = tensors[i].grad_bf16 ? 1 : 0;
+    b.grad[count] = low32(tensors[i].grad) | (tensors[i].grad_bf16 ? 1u : 0u);
+    b.n[count] = (uint32_t)tensors[i].n;
+    b.upper[count / 2] |= upper16(tensors[i].grad) << (16 * (count & 1));
     b.begin[count++] = b.chunks;
     b.chunks += (uint32_t)chunks;
   }
@@ -434,9 +449,7 @@ hilore_status hilore_adamw(const hilore_adamw_tensor *tensors, int n_tensors, do
   const double c1 = 1.0 - std::pow(beta1, (double)step);
   const double c2 = 1.0 - std::pow(beta2, (double)step);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  int count = 0;
-  hilore::AdamwBatch b{};
-  clear(b, count);
+  hilore::AdamwBatch b;
   b.norm = norm;
   b.beta1 = (float)beta1;
   b.one_beta1 = (float)(1.0 - beta1);
@@ -444,33 +457,59 @@ hilore_status hilore_adamw(const hilore_adamw_tensor *tensors, int n_tensors, do
   b.one_beta2 = (float)(1.0 - beta2);
   b.eps = (float)eps;
   b.inv_sqrt_c2 = (float)(1.0 / std::sqrt(c2));
+  b.seed = seed;
+  bool has_p = false, has_p16 = false, has_scales = false;
+  for (int i = 0; i < n_tensors; ++i) {
+    if (tensors[i].n == 0) continue;
+    has_p |= tensors[i].p != nullptr;
+    has_p16 |= tensors[i].p16 != nullptr;
+    has_scales |= tensors[i].m_scales != nullptr;
+  }
+  b.has_p = has_p;
+  b.has_p16 = has_p16;
+  b.stride = 9 + (has_p && has_p16 ? 2 : 0) + (has_scales ? 3 : 0);
+  b.cap = hilore::kAdamwWords / (b.stride + 1);
+  int count;
+  clear(b, count);
+  // one without elements keeps its number and gets no workgroup
   for (int i = 0; i < n_tensors; ++i) {
     const hilore_adamw_tensor &t = tensors[i];
-    if (t.n == 0) continue;
     const int64_t chunks = (t.n + hilore::kAdamwChunk - 1) / hilore::kAdamwChunk;
-    if (count == hilore::kAdamwPerLaunch || (count > 0 && b.chunks + chunks > kMaxChunks)) {
-      st = hip_status(hilore::launch_adamw(b, s));
-      if (st != HILORE_OK) return st;
+    if (count == b.cap || (b.chunks > 0 && b.chunks + chunks > kMaxChunks)) {
+      if (b.chunks > 0) {
+        st = hip_status(hilore::launch_adamw(b, s));
+        if (st != HILORE_OK) return st;
+      }
       clear(b, count);
     }
-    hilore::AdamwTensor &o = b.t[count];
-    o.p = t.p;
-    o.p16 = t.p16;
-    o.grad = t.grad;
-    o.m = t.m;
-    o.v = t.v;
-    o.m_scales = t.m_scales;
-    o.v_scales = t.v_scales;
-    o.n = t.n;
-    o.step_size = (float)((double)t.lr / c1);
-    o.decay = (float)(1.0 - (double)t.lr * (double)t.weight_decay);
-    o.key_state = hilore::adamw_key(seed, i, 0u);
-    o.key_param = hilore::adamw_key(seed, i, 0x3C6EF372u);
-    o.grad16 = t.grad_bf16 ? 1 : 0;
-    b.begin[count++] = b.chunks;
+    if (count == 0) b.first = i;
+    uint32_t *rec = b.w + b.cap + count * b.stride;
+    if (t.n > 0) {
+      rec[0] = low32(t.grad) | (t.grad_bf16 ? 1u : 0u);
+      rec[1] = low32(t.m);
+      rec[2] = low32(t.v);
+      rec[3] = upper16(t.grad) | upper16(t.m) << 16;
+      rec[4] = (uint32_t)t.n;
+      const void *param = has_p ? (const void *)t.p : t.p16;
+      rec[5] = upper16(t.v) | upper16(param) << 16;
+      rec[6] = low32(param);
+      rec[7] = __builtin_bit_cast(uint32_t, (float)((double)t.lr / c1));
+      rec[8] = __builtin_bit_cast(uint32_t, (float)(1.0 - (double)t.lr * (double)t.weight_decay));
+      uint32_t *next = rec + 9;
+      if (has_p && has_p16) {
+        *next++ = low32(t.p16);
+        *next++ = upper16(t.p16);
+      }
+      if (has_scales) {
+        *next++ = low32(t.m_scales);
+        *next++ = low32(t.v_scales);
+        *next = upper16(t.m_scales) | upper16(t.v_scales) << 16;
+      }
+    }
+    b.w[count++] = b.chunks;
     b.chunks += (uint32_t)chunks;
   }
-  return count > 0 ? hip_status(hilore::launch_adamw(b, s)) : HILORE_OK;
+  return b.chunks > 0 ? hip_status(hilore::launch_adamw(b, s)) : HILORE_OK;
 }
 
 }  // extern "C"

@@ -188,6 +188,18 @@ __device__ __forceinline__ void roots(const float v[E], float r[E]) {
   }
 }
 
+struct AdamwTensor {
+  float *p;
+  uint16_t *p16;
+  const void *grad;
+  void *m, *v;
+  float *m_scales, *v_scales;
+  int64_t n;
+  float step_size, decay;
+  uint32_t key_state, key_param;
+  int grad16;
+};
+
 struct Scalars {
   float beta1, one_beta1, beta2, one_beta2, eps, inv_sqrt_c2, clip;
 };
@@ -345,29 +357,79 @@ __device__ __forceinline__ void step_any(const AdamwTensor &t, int64_t begin, co
 }
 
 // Tensor of workgroup `b`: the last whose chunks begin at or before it (unused entries of
-// `begin` are 2^32 - 1).  Every lane looks at one tensor of 64, so there is one load's wait,
-// where a binary search has one a step (233M elements, 8 bit: 560 -> 430 us with the step's
-// instructions cut; by unrolled scalar loads 463).
+// `begin` are 2^32 - 1; one without elements begins where the next one does).  Every lane looks
+// at one tensor of 64, so there is one load's wait, where a binary search has one a step (233M
+// elements, 8 bit: 560 -> 430 us with the step's instructions cut; by unrolled scalar loads 463).
 template <int N>
-__device__ __forceinline__ int tensor_of(const uint32_t *begin, uint32_t b) {
+__device__ __forceinline__ int tensor_of(const uint32_t *begin, int count, uint32_t b) {
   int before = 0;
 #pragma unroll
   for (int j = 0; j < N; j += kWave) {
     const int i = j + (int)(threadIdx.x & 63);
-    before += __popcll(__ballot(i < N && begin[i < N ? i : 0] <= b));
+    const uint32_t first = begin[i < count ? i : 0];
+    before += __popcll(__ballot((i < count) & (first <= b)));
   }
   return before - 1;
 }
 
-__global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamwBatch a) {
-  float clip = 1.0f;
-  if (a.norm) {
-    clip = a.norm[1];
-    if (!(clip <= 1.0f)) return;  // NaN: the step is skipped
-  }
-  const int k = tensor_of<kAdamwPerLaunch>(a.begin, blockIdx.x);
-  const AdamwTensor &t = a.t[k];
-  const int64_t begin = ((int64_t)blockIdx.x - a.begin[k]) * kAdamwChunk;
+// Key of the random bits of tensor `index` of a call.
+__device__ __forceinline__ uint32_t adamw_key(uint32_t seed, int index, uint32_t salt) {
+  return mix32(seed + 0x9E3779B1u * (uint32_t)(index + 1) + salt);
+}
+
+// Global memory, not whatever address space: a pointer made of words says nothing of it, and the
+// accesses would be flat ones (233M elements, 8 bit: 594 us a step with its norm, so 562).
+template <typename T>
+__device__ __forceinline__ T *global_at(uint64_t a) {
+  return (T *)(__attribute__((address_space(1))) T *)a;
+}
+
+// Tensor k of a launch; its whole record is read at once (a shorter one with some of what
+// follows it in the batch).
+__device__ __forceinline__ AdamwTensor tensor_at(const AdamwBatch &a, int k, float clip) {
+  const uint32_t *rec = a.w + a.cap + k * a.stride;
+  uint32_t r[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) r[i] = rec[i];
+  // all of them in one wait: each load on its own is a trip to the host's memory
+  asm volatile("" ::"s"(r[0]), "s"(r[1]), "s"(r[2]), "s"(r[3]), "s"(r[4]), "s"(r[5]), "s"(r[6]), "s"(r[7]),
+               "s"(r[8]), "s"(r[9]), "s"(r[10]), "s"(r[11]), "s"(r[12]), "s"(r[13]), "s"(a.w[k]), "s"(a.eps),
+               "s"(a.first), "s"(clip));
+  const auto pointer = [](uint32_t low, uint32_t upper) { return (uint64_t)(upper & 0xFFFFu) << 32 | low; };
+  const bool both = a.has_p && a.has_p16;
+  const bool scales = a.stride > (both ? 11 : 9);
+  const uint64_t param = pointer(r[6], r[5] >> 16), second = pointer(r[9], r[10]);
+  const uint32_t low_m = both ? r[11] : r[9], low_v = both ? r[12] : r[10], upper = both ? r[13] : r[11];
+  AdamwTensor t;
+  t.p = global_at<float>(a.has_p ? param : 0);
+  t.p16 = global_at<uint16_t>(both ? second : a.has_p ? 0 : param);
+  t.grad = global_at<const uint8_t>(pointer(r[0] & ~15u, r[3]));
+  t.grad16 = (int)(r[0] & 1u);
+  t.m = global_at<uint8_t>(pointer(r[1], r[3] >> 16));
+  t.v = global_at<uint8_t>(pointer(r[2], r[5]));
+  t.m_scales = global_at<float>(scales ? pointer(low_m, upper) : 0);
+  t.v_scales = global_at<float>(scales ? pointer(low_v, upper >> 16) : 0);
+  t.n = (int64_t)r[4];
+  t.step_size = __uint_as_float(r[7]);
+  t.decay = __uint_as_float(r[8]);
+  t.key_state = adamw_key(a.seed, a.first + k, 0u);
+  t.key_param = adamw_key(a.seed, a.first + k, 0x3C6EF372u);
+  return t;
+}
+
+// Five waves a SIMD, with some spills in the kinds of most operands (a step with its norm: 28
+// adapters in 8 bit 16.3 -> 14.0 us, 233M elements 564 -> 554).  By the tensors' packing into
+// fewer launches, 343 of 215 elements: 85 -> 65 us, 392 adapters of 40M elements 304 -> 268.
+__device__ const float kNoClip[2] = {0.0f, 1.0f};
+
+__global__ __launch_bounds__(kThreads, 5) void adamw_kernel(const AdamwBatch a) {
+  // a uniform load, asked for before the tensors' first chunks are there
+  const uintptr_t norm = reinterpret_cast<uintptr_t>(a.norm ? a.norm : kNoClip);
+  const float clip = reinterpret_cast<const __attribute__((address_space(4))) float *>(norm)[1];
+  const int k = __builtin_amdgcn_readfirstlane(tensor_of<128>(a.w, a.cap, blockIdx.x));
+  const AdamwTensor t = tensor_at(a, k, clip);
+  const int64_t begin = ((int64_t)blockIdx.x - a.w[k]) * kAdamwChunk;
+  if (!(clip <= 1.0f)) return;  // NaN: the step is skipped
   const Scalars s = {a.beta1, a.one_beta1, a.beta2,
                      a.one_beta2, a.eps, a.inv_sqrt_c2, clip};
   const int param = t.p ? (t.p16 ? 1 : 0) : 2;
@@ -424,14 +486,15 @@ __device__ __forceinline__ double chunk_squares(const T *g, int64_t n, int64_t b
 
 __global__ __launch_bounds__(kThreads) void norm_partial_kernel(const NormBatch a) {
   __shared__ double lds[kThreads / kWave];
-  const int k = tensor_of<kNormPerLaunch>(a.begin, blockIdx.x);
-  const NormTensor &t = a.t[k];
-  const int64_t chunk = kNormChunkBytes / (t.grad16 ? 2 : 4);  // elements
-  const int64_t begin = ((int64_t)blockIdx.x - a.begin[k]) * chunk, n = t.n;
+  const int k = tensor_of<kNormPerLaunch>(a.begin, kNormPerLaunch, blockIdx.x);
+  const bool grad16 = a.grad[k] & 1u;
+  const uint64_t at = (uint64_t)(a.upper[k / 2] >> (16 * (k & 1)) & 0xFFFFu) << 32 | (a.grad[k] & ~15u);
+  const int64_t chunk = kNormChunkBytes / (grad16 ? 2 : 4);  // elements
+  const int64_t begin = ((int64_t)blockIdx.x - a.begin[k]) * chunk, n = a.n[k];
   const bool full = begin + chunk <= n;
-  const float *g = static_cast<const float *>(t.grad);
-  const uint16_t *g16 = static_cast<const uint16_t *>(t.grad);
-  double sum = t.grad16 ? (full ? chunk_squares<true>(g16, n, begin) : chunk_squares<false>(g16, n, begin))
+  const float *g = global_at<const float>(at);
+  const uint16_t *g16 = global_at<const uint16_t>(at);
+  double sum = grad16 ? (full ? chunk_squares<true>(g16, n, begin) : chunk_squares<false>(g16, n, begin))
                         : (full ? chunk_squares<true>(g, n, begin) : chunk_squares<false>(g, n, begin));
   sum = group_sum(sum, lds);
   if (threadIdx.x == 0) a.part[blockIdx.x] = sum;
@@ -475,16 +538,6 @@ hipError_t launch_norm_fold(const double *part, int64_t n, float max_norm, float
                             hipStream_t s) {
   hipLaunchKernelGGL(norm_fold_kernel, dim3(1), dim3(kFoldThreads), 0, s, part, n, max_norm, norm);
   return hipGetLastError();
-}
-
-// Key of the random bits of tensor `index` of a call.
-uint32_t adamw_key(uint32_t seed, int index, uint32_t salt) {
-  uint32_t x = seed + 0x9E3779B1u * (uint32_t)(index + 1) + salt;
-  x ^= x >> 16;
-  x *= 0x6A09E667u;
-  x ^= x >> 15;
-  x *= 0xBB67AE85u;
-  return x ^ (x >> 16);
 }
 
 }  // namespace hilore

@@ -281,41 +281,35 @@ hipError_t launch_swiglu_bwd(const SwigluArgs &a, int code, int block, hipStream
 // chunks.
 constexpr int kAdamwBlock = 256;          // elements per scale of an 8-bit state
 constexpr int64_t kAdamwChunk = 4096;     // elements per workgroup
-constexpr int kAdamwPerLaunch = 44;
-struct AdamwTensor {
-  float *p;
-  uint16_t *p16;
-  const void *grad;
-  void *m, *v;
-  float *m_scales, *v_scales;
-  int64_t n;
-  float step_size, decay;  // lr / (1 - beta1^step), 1 - lr * weight_decay
-  uint32_t key_state, key_param;
-  int grad16;
-};
+// Tensors travel in the kernel arguments, 4 KB a launch, packed into words: the first chunks
+// [cap], then records [cap][stride] of 9 to 14 words, with 48 bits of each pointer that any
+// tensor of the call has:
+//   0 grad (bit 0: bf16)  1 m  2 v  3 upper halves of grad and m  4 n  5 upper halves of v and
+//   param  6 param (p, else p16)  7 step size lr / (1 - beta1^step)  8 decay 1 - lr * weight_decay
+//   with both p and p16:  p16 and its upper half;  with 8-bit states:  m_scales, v_scales and
+//   their upper halves
+constexpr int kAdamwWords = 1008;
 struct AdamwBatch {
-  AdamwTensor t[kAdamwPerLaunch];
-  uint32_t begin[kAdamwPerLaunch];  // first chunk of each tensor, then 2^32 - 1
-  uint32_t chunks;
+  uint32_t w[kAdamwWords];
   const float *norm;
   float beta1, one_beta1, beta2, one_beta2, eps, inv_sqrt_c2;
+  uint32_t seed;
+  int first;  // number of the first tensor in the call
+  int cap, stride, has_p, has_p16;
+  uint32_t chunks;
 };
 static_assert(sizeof(AdamwBatch) <= 4096, "kernel arguments");
 hipError_t launch_adamw(const AdamwBatch &a, hipStream_t s);
-uint32_t adamw_key(uint32_t seed, int index, uint32_t salt);
 
 constexpr int64_t kNormChunkBytes = 32768;  // of a gradient per workgroup
-constexpr int kNormPerLaunch = 192;
-struct NormTensor {
-  const void *grad;
-  uint32_t n;  // < 2^32
-  uint32_t grad16;
-};
+constexpr int kNormPerLaunch = 288;
 struct NormBatch {
-  NormTensor t[kNormPerLaunch];
-  uint32_t begin[kNormPerLaunch];
+  uint32_t begin[kNormPerLaunch];  // first chunk of each gradient, then 2^32 - 1
+  uint32_t grad[kNormPerLaunch];   // low words of the pointers; bit 0: bf16
+  uint32_t n[kNormPerLaunch];      // < 2^32
+  uint32_t upper[kNormPerLaunch / 2];  // bits 32 to 47 of the pointers, two to a word
+  double *part;                    // partial sums of this launch's chunks
   uint32_t chunks;
-  double *part;  // partial sums of this launch's chunks
 };
 static_assert(sizeof(NormBatch) <= 4096, "kernel arguments");
 hipError_t launch_norm_partial(const NormBatch &a, hipStream_t s);

@@ -200,3 +200,10 @@ def test_int8_output_size(lib):  # noqa: F811
         assert product(lib, quantize, tokens=1 << 30, n=2048, ldo=2048) == UNSUP
         d = make(E.hilore_int8_desc, dict(tokens=1 << 30, n=2048, k=64), {})
         assert lib.hilore_int8_workspace_bytes(ctypes.byref(d), int(quantize)) == 0
+
+
+@pytest.mark.parametrize("field", ["p", "p16", "grad", "m", "v", "m_scales", "v_scales"])
+def test_adamw_addresses(lib, field):  # noqa: F811
+    """Addresses travel as 48 bits: others are refused, wherever they stand."""
+    kw = dict(p=FAKE, p16=FAKE, m_scales=FAKE, v_scales=FAKE) | {field: 1 << 48}
+    assert adamw(lib, [tensor(), tensor(**kw)]) == UNSUP
