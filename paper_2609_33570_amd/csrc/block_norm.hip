@@ -542,9 +542,11 @@ hipError_t launch_block_norm(const BlockNormArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Workgroups of the backward kernel.  With sums over rows each writes a row of them and the
-// fold reads it, 24 B a column: at least four turns a workgroup pay for it (512 x 3584 in 512
-// workgroups 25 us).
+// Workgroups of the backward kernel.  With sums over rows each writes a row of them and the fold
+// reads it, 24 B a column at some 4 TB/s; a turn of a workgroup takes about 1.5 us and 1 us more
+// every 2200 columns.  So turns / groups + groups * row is least at the root below (with
+// four turns for each workgroup 10 x 16128 took 37 us, now 16; 97 x 10112 37 and 19, 123 x 288 13.6 and
+// 8.1; 512 x 3584 18 and 15, and in 512 workgroups 25).
 int block_norm_bwd_groups(int64_t rows, int64_t cols, int sums) {
   if (cols == 0 || rows == 0) return 0;
   int threads, pieces;
@@ -552,8 +554,9 @@ int block_norm_bwd_groups(int64_t rows, int64_t cols, int sums) {
   const int side = side_rows(threads);
   const int full = row_groups(rows, threads, side, pieces == 1 ? 2 * kMaxWaves : kMaxWaves);
   if (!sums) return full;
-  const int64_t turns = (rows + 4 * side - 1) / (4 * side);
-  return turns < full ? (int)turns : full;
+  const double turns = (double)rows / side * (1.5 + (double)cols / 2200), row = (double)cols * 24 / 4e6;
+  const double best = __builtin_sqrt(turns / row);
+  return best < full ? (best < 1.0 ? 1 : (int)best) : full;
 }
 
 hipError_t launch_block_norm_bwd(const BlockNormBwdArgs &a, hipStream_t s) {
