@@ -14,7 +14,8 @@
 // is (bits + 20 random bits) >> 20; the hash gives the upper 16 of them.
 //
 // Bound by HBM: per element 28 B with everything in fp32 (p, m, v read and
-// written, g read), 10 B with bf16 parameters and gradients and 8-bit states.
+// written, g read), 10 B with bf16 parameters and gradients and 8-bit states.  The step runs at
+// 5.3 TB/s of those bytes (40M fp32 elements 210 us, 233M with 8-bit states 440), the norm at 3.9.
 #include "device_common.hpp"
 #include "hilore_internal.hpp"
 

