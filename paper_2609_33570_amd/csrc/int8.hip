@@ -428,12 +428,18 @@ struct TileScales {
   uint16_t bias[Tile<B>::kSide];
 };
 
+// Rows of a tile of S from `at` on: 0 in a quarter (see below) past the operand.
+template <int S>
+__device__ __forceinline__ int64_t rows_left(int64_t rows, int64_t at) {
+  const int64_t left = rows - at;
+  return left < S ? (left > 0 ? left : 0) : S;
+}
+
 template <int B>
 __device__ __forceinline__ void dma_scales(const Int8Args &a, int64_t t0, int64_t n0,
                                            TileScales<B> &s, int wave, int lane) {
   constexpr int S = Tile<B>::kSide;
-  const int64_t rows_t = a.tokens - t0 < S ? a.tokens - t0 : S;
-  const int64_t rows_n = a.n - n0 < S ? a.n - n0 : S;
+  const int64_t rows_t = rows_left<S>(a.tokens, t0), rows_n = rows_left<S>(a.n, n0);
   const auto copy = [&](const void *from, int64_t bytes, void *to) {
     const __amdgpu_buffer_rsrc_t r =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(from), 0, (int)bytes, 0x00020000);
@@ -532,11 +538,14 @@ __device__ __forceinline__ void tile_store(const i32x16 (&acc)[B][B], const Int8
 // of 8 x 4 tiles.  An XCD's workgroups have a block and share its rows in their L2, and the blocks
 // at work at a time make up 16 x 16 tiles, whose rows come from memory once for all XCDs (with
 // rows of tiles to each XCD of their own 16384 x 3584 x 18944 takes 1166 us, so 1080).
-template <int B>
+// QUARTERS: the tiles are of 256 x 256 and a piece is a quarter of one.
+template <int B, bool QUARTERS>
 __device__ __forceinline__ TileWork work_of(const Int8Args &a, int id, int tiles_t, int tiles_n,
                                             int parts) {
   const int tiles = tiles_t * tiles_n;
   TileWork w;
+  const int quarter = id & 3;
+  if constexpr (QUARTERS) id >>= 2;
   w.part = __builtin_amdgcn_readfirstlane(id / tiles);
   id -= w.part * tiles;
   const int group = id / (kGroupT * tiles_n), t_first = group * kGroupT;
@@ -549,8 +558,8 @@ __device__ __forceinline__ TileWork work_of(const Int8Args &a, int id, int tiles
   const int bt = gt - block * kBlockT < kBlockT ? gt - block * kBlockT : kBlockT;
   id -= block * kBlockT * gn;
   const int t = t_first + block * kBlockT + id % bt, n = n_first + id / bt;
-  w.t0 = (int64_t)__builtin_amdgcn_readfirstlane(t) * Tile<B>::kSide;
-  w.n0 = (int64_t)__builtin_amdgcn_readfirstlane(n) * Tile<B>::kSide;
+  w.t0 = (int64_t)__builtin_amdgcn_readfirstlane(QUARTERS ? 2 * t + (quarter & 1) : t) * Tile<B>::kSide;
+  w.n0 = (int64_t)__builtin_amdgcn_readfirstlane(QUARTERS ? 2 * n + (quarter >> 1) : n) * Tile<B>::kSide;
   const int turns = (a.k + kTurnK - 1) / kTurnK;  // <= 2^9, of at most 2^8 parts
   w.begin = turns * w.part / parts * kTurnK;
   const int end = turns * (w.part + 1) / parts * kTurnK;
@@ -561,8 +570,7 @@ __device__ __forceinline__ TileWork work_of(const Int8Args &a, int id, int tiles
 template <int B>
 __device__ __forceinline__ TileSource tile_source(const Int8Args &a, const TileWork &w) {
   constexpr int S = Tile<B>::kSide;
-  const int64_t rows_t = a.tokens - w.t0 < S ? a.tokens - w.t0 : S;
-  const int64_t rows_n = a.n - w.n0 < S ? a.n - w.n0 : S;
+  const int64_t rows_t = rows_left<S>(a.tokens, w.t0), rows_n = rows_left<S>(a.n, w.n0);
   TileSource s;
   s.a = __builtin_amdgcn_make_buffer_rsrc((void *)(a.a + w.t0 * a.k), 0, (int)(rows_t * a.k), 0x00020000);
   s.b = __builtin_amdgcn_make_buffer_rsrc((void *)(a.w + w.n0 * a.k), 0, (int)(rows_n * a.k), 0x00020000);
@@ -572,9 +580,10 @@ __device__ __forceinline__ TileSource tile_source(const Int8Args &a, const TileW
 // A workgroup stays for its pieces of all rounds.  Their stages follow one another in the ring
 // without a gap: while a piece's last four are multiplied, the next one's first four
 // are loaded, and they land while the outputs are written.
-template <int B, int MODE>
-__global__ __launch_bounds__(kTileThreads, Tile<B>::kPerCu) void int8_tile_kernel(const Int8Args a, int tiles_t,
-                                                                    int tiles_n, int parts) {
+// It has the pieces from `first` to `first` + `pieces`.
+template <int B, int MODE, bool QUARTERS>
+__global__ __launch_bounds__(kTileThreads, Tile<B>::kPerCu) void int8_tile_kernel(
+    const Int8Args a, int tiles_t, int tiles_n, int parts, int first, int pieces) {
   constexpr int kBytes = Tile<B>::kStageBytes;
   __shared__ __attribute__((aligned(16))) uint8_t a0[kBytes], b0[kBytes], a1[kBytes], b1[kBytes];
   __shared__ __attribute__((aligned(16))) uint8_t a2[kBytes], b2[kBytes], a3[kBytes], b3[kBytes];
@@ -583,11 +592,11 @@ __global__ __launch_bounds__(kTileThreads, Tile<B>::kPerCu) void int8_tile_kerne
 
   // every round of the grid takes the next gridDim.x pieces, XCD x (workgroups are dealt round
   // robin) an eighth of them; -1: no more
-  const int pieces = tiles_t * tiles_n * parts, x = blockIdx.x & 7, slot = blockIdx.x >> 3;
+  const int x = blockIdx.x & 7, slot = blockIdx.x >> 3;
   const auto piece = [&](int begin) {
     const int count = pieces - begin < (int)gridDim.x ? pieces - begin : (int)gridDim.x;
     const int per = count >> 3, more = count & 7;
-    return slot < per + (x < more ? 1 : 0) ? begin + x * per + (x < more ? x : more) + slot : -1;
+    return slot < per + (x < more ? 1 : 0) ? first + begin + x * per + (x < more ? x : more) + slot : -1;
   };
   int begin = 0, id = piece(0);  // the grid is at most the pieces: every workgroup has one
 
@@ -613,7 +622,7 @@ __global__ __launch_bounds__(kTileThreads, Tile<B>::kPerCu) void int8_tile_kerne
     ob[ks] = o + (uint32_t)(wn * 32 * B * kStageK);
   }
 
-  TileWork w = work_of<B>(a, id, tiles_t, tiles_n, parts), next = w;
+  TileWork w = work_of<B, QUARTERS>(a, id, tiles_t, tiles_n, parts), next = w;
   TileSource src = tile_source<B>(a, w);
   dma_stage(src, tl, w.begin, w.end, a0, b0, wave);
   dma_stage(src, tl, w.begin + kStageK, w.end, a1, b1, wave);
@@ -644,7 +653,7 @@ __global__ __launch_bounds__(kTileThreads, Tile<B>::kPerCu) void int8_tile_kerne
         id = begin < pieces ? piece(begin) : -1;
         more_work = id >= 0;
         if (more_work) {
-          next = work_of<B>(a, id, tiles_t, tiles_n, parts);
+          next = work_of<B, QUARTERS>(a, id, tiles_t, tiles_n, parts);
           src = tile_source<B>(a, next);
           at = next.begin;
         } else {
@@ -734,11 +743,16 @@ void launch_few(const Int8Args &a, const FewPlan &p, hipStream_t s) {
 // of all of k or of one of several parts of it.  The larger tile reads half as much per product
 // and wins where there are tiles for all CUs; the smaller one, parts of k, or both, where there
 // are not: 700 x 3584 x 3584 takes 18.4 us in small tiles and 44.0 in large ones,
-// 3000 x 3584 x 3584 54.7 and 50.8; 128 x 18944 x 3584 118 us whole and 28 in nine parts.  The plan
-// with the least estimated time is taken.  The estimate, in us, was fitted to both sides and 1, 2
-// and 4 parts at 39 shapes of 65 to 16384 tokens, of which it takes one within 5 % of the fastest.
+// 3000 x 3584 x 3584 54.7 and 50.8; 128 x 18944 x 3584 118 us whole and 28 in nine parts.  The
+// plan with the least estimated time is taken.  The estimate, in us, was fitted to both sides and
+// 1, 2 and 4 parts at 39 shapes of 65 to 16384 tokens; it takes one within about 5 % of the fastest.
+// Where 256 x 256 tiles leave a last round with at most 64, those may go as quarters of 128 x 128,
+// one to a CU, in a launch of their own (4200 x 4112 x 4104, 33 tiles: 136 -> 102 us,
+// 1789 x 4864 x 18944, 6: 215 -> 191).  Half a round stays as it is (16384 x 18944 x 3584 1069, as
+// quarters 1104): under the power limit half the CUs run faster.
 struct TilePlan {
   int side, parts;
+  int64_t quartered;  // of the last tiles of 256 x 256
 };
 
 constexpr int kMaxParts = 32;
@@ -746,18 +760,27 @@ constexpr int kMaxParts = 32;
 TilePlan tile_plan(int64_t tokens, int64_t k, int64_t n) {
   const int64_t turns = (k + kTurnK - 1) / kTurnK;
   const double far = k * n > (int64_t)1 << 25 ? 1.4 : 1.0;  // weights from beyond the caches
-  TilePlan best{256, 1};
+  TilePlan best{256, 1, 0};
   double least = 0.0;
   for (const int side : {256, 128}) {
     const double stage = (side == 256 ? 0.55 : 0.22) * far, ends = side == 256 ? 5.0 : 2.0;
-    const int64_t tiles = ((tokens + side - 1) / side) * ((n + side - 1) / side);
+    const int64_t tiles = ((tokens + side - 1) / side) * ((n + side - 1) / side), rest = tiles % 256;
     for (int parts = 1; parts == 1 || (parts <= turns && parts <= kMaxParts); ++parts) {
       const int64_t rounds = (tiles * parts + 255) / 256;
       double us = ends + (double)rounds * ((double)((turns + parts - 1) / parts) * 4 * stage + ends);
       if (parts > 1) us += 3.0 + parts * (0.5 + (double)tokens * (double)n * 8 / 6e6);
       if (least == 0.0 || us < least) {
         least = us;
-        best = TilePlan{side, parts};
+        best = TilePlan{side, parts, 0};
+      }
+      if (side == 256 && parts == 1 && rest > 0 && rest <= 64 && rest < tiles) {
+        const double whole = (double)(turns * 4) * stage + ends;
+        const double quarter = (double)(turns * 4) * 0.22 * far + 2.0;
+        us = ends + (double)(rounds - 1) * whole + 6.0 + (double)((4 * rest + 255) / 256) * quarter;
+        if (us < least) {
+          least = us;
+          best = TilePlan{256, 1, rest};
+        }
       }
       if (rounds > 4) break;  // work enough for every CU
     }
@@ -765,20 +788,24 @@ TilePlan tile_plan(int64_t tokens, int64_t k, int64_t n) {
   return best;
 }
 
-template <int B>
-void launch_tiles(const Int8Args &a, const TilePlan &p, hipStream_t s) {
-  constexpr int S = Tile<B>::kSide;
+template <int B, bool QUARTERS>
+void launch_tiles(const Int8Args &a, int64_t first, int64_t pieces, int parts, hipStream_t s) {
+  constexpr int S = QUARTERS ? 256 : Tile<B>::kSide;
   const int tiles_t = (int)((a.tokens + S - 1) / S), tiles_n = (int)((a.n + S - 1) / S);
-  const int64_t pieces = (int64_t)tiles_t * tiles_n * p.parts;
   constexpr int64_t kResident = 256 * Tile<B>::kPerCu;
   const dim3 grid((unsigned)(pieces < kResident ? pieces : kResident)), block(kTileThreads);
-  if (p.parts > 1) {
-    hipLaunchKernelGGL((int8_tile_kernel<B, kStorePart>), grid, block, 0, s, a, tiles_t, tiles_n, p.parts);
-    launch_join(a, p.parts, s);
+  if (parts > 1) {
+    if constexpr (!QUARTERS) {
+      hipLaunchKernelGGL((int8_tile_kernel<B, kStorePart, false>), grid, block, 0, s, a, tiles_t, tiles_n,
+                         parts, 0, (int)pieces);
+      launch_join(a, parts, s);
+    }
   } else if (a.out_f32 || a.accumulate) {
-    hipLaunchKernelGGL((int8_tile_kernel<B, kStoreWide>), grid, block, 0, s, a, tiles_t, tiles_n, 1);
+    hipLaunchKernelGGL((int8_tile_kernel<B, kStoreWide, QUARTERS>), grid, block, 0, s, a, tiles_t, tiles_n, 1,
+                       (int)first, (int)pieces);
   } else {
-    hipLaunchKernelGGL((int8_tile_kernel<B, kStoreBf16>), grid, block, 0, s, a, tiles_t, tiles_n, 1);
+    hipLaunchKernelGGL((int8_tile_kernel<B, kStoreBf16, QUARTERS>), grid, block, 0, s, a, tiles_t, tiles_n, 1,
+                       (int)first, (int)pieces);
   }
 }
 
@@ -801,8 +828,13 @@ hipError_t launch_int8(const Int8Args &a, hipStream_t s) {
     return hipGetLastError();
   }
   const TilePlan p = tile_plan(a.tokens, a.k, a.n);
-  if (p.side == 256) launch_tiles<4>(a, p, s);
-  else launch_tiles<2>(a, p, s);
+  const int64_t tiles = ((a.tokens + p.side - 1) / p.side) * ((a.n + p.side - 1) / p.side);
+  if (p.side == 128) {
+    launch_tiles<2, false>(a, 0, tiles * p.parts, p.parts, s);
+  } else {
+    launch_tiles<4, false>(a, 0, (tiles - p.quartered) * p.parts, p.parts, s);
+    if (p.quartered > 0) launch_tiles<2, true>(a, (tiles - p.quartered) * 4, p.quartered * 4, 1, s);
+  }
   return hipGetLastError();
 }
 

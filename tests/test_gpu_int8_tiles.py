@@ -87,3 +87,26 @@ def test_no_depth(hl, tokens):
                                        a=torch.empty(tokens, 0, dtype=torch.int8, device="cuda"),
                                        a_scales=torch.ones(tokens, device="cuda"), bias=bias))
     assert torch.equal(out, bias.expand(tokens, n))
+
+
+@pytest.mark.parametrize("tokens,k,n", [(4200, 4112, 4104), (4400, 2064, 4104), (1789, 4864, 18944), (6167, 1616, 9480)])
+@pytest.mark.parametrize("out_f32,accumulate", [(False, False), (True, False), (False, True)])
+def test_last_tiles_in_quarters(hl, tokens, k, n, out_f32, accumulate):
+    """A last round of few large tiles goes as quarters, some of which lie past the operands."""
+    a, w = random_codes(tokens, tokens, k), random_codes(n, n, k)
+    g = torch.Generator(device="cuda").manual_seed(k)
+    sa = torch.rand(tokens, generator=g, device="cuda") * 1e-2 + 1e-4
+    sw = torch.rand(n, generator=g, device="cuda") * 1e-2 + 1e-4
+    bias = torch.randn(n, generator=g, device="cuda").bfloat16()
+    out0 = torch.randn(tokens + 3, n + 8, generator=g, device="cuda").to(torch.float32 if out_f32 else torch.bfloat16)
+    out = out0.clone()
+    hl.hilore_int8_matmul(hl.int8_desc(w=w, out=out[:tokens, :n], a=a, a_scales=sa, w_scales=sw, bias=bias,
+                                       accumulate=accumulate))
+    want = sums(a, w) * sa.double()[:, None] * sw.double()
+    size = want.abs() + bias.double().abs()
+    want = want + bias.double()
+    if accumulate:
+        want, size = want + out0[:tokens, :n].double(), size + out0[:tokens, :n].double().abs()
+    tol = 5 * U * size + (0.0 if out_f32 else 2.0 ** -8 * want.abs())
+    assert ((out[:tokens, :n].double() - want).abs() <= tol).all()
+    assert torch.equal(out[:, n:], out0[:, n:]) and torch.equal(out[tokens:], out0[tokens:])
