@@ -298,7 +298,8 @@ __global__ __launch_bounds__(WAVES * 64) void int8_few_kernel(const Int8Args a, 
 
 // The sums of `parts` partial products ([part][token][channel] in the workspace).
 __global__ __launch_bounds__(256) void int8_join_kernel(const Int8Args a, int parts) {
-  const uint32_t quads = (uint32_t)a.n / 4, all = (uint32_t)a.tokens * quads;  // < 64 * 2^24
+  const uint32_t quads = (uint32_t)a.n / 4, all = (uint32_t)a.tokens * quads;
+  // < 2^31: 64 tokens of 2^24 quads, or 1024 tiles, more of which are not split
   for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) {
     const i32x4 *p = reinterpret_cast<const i32x4 *>(a.part) + i;
     i32x4 sum = *p;
