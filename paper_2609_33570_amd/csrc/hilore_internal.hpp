@@ -301,7 +301,7 @@ struct AdamwBatch {
 static_assert(sizeof(AdamwBatch) <= 4096, "kernel arguments");
 hipError_t launch_adamw(const AdamwBatch &a, hipStream_t s);
 
-constexpr int64_t kNormChunkBytes = 32768;  // of a gradient per workgroup
+constexpr int64_t kNormChunkBytes = 16384;  // of a gradient per workgroup
 constexpr int kNormPerLaunch = 288;
 struct NormBatch {
   uint32_t begin[kNormPerLaunch];  // first chunk of each gradient, then 2^32 - 1
