@@ -228,9 +228,13 @@ __device__ __forceinline__ void load_piece(Piece<EIGHT, GRAD16, PARAM> &x, const
   if constexpr (EIGHT) {
     load_lane<FULL>(x.mc, static_cast<const uint8_t *>(t.m), i, n);
     load_lane<FULL>(x.vc, static_cast<const uint8_t *>(t.v), i, n);
-    const int64_t block = FULL || n > 0 ? i / kAdamwBlock : 0;
-    x.ms = t.m_scales[block];
-    x.vs = t.v_scales[block];
+    // a lane past the end still takes part in its block's largest value: with zeros, whatever
+    // another block's scale may be
+    x.ms = x.vs = 0.0f;
+    if (FULL || n > 0) {
+      x.ms = t.m_scales[i / kAdamwBlock];
+      x.vs = t.v_scales[i / kAdamwBlock];
+    }
   } else {
     load_lane<FULL>(x.m, static_cast<const float *>(t.m), i, n);
     load_lane<FULL>(x.v, static_cast<const float *>(t.v), i, n);
