@@ -341,7 +341,8 @@ hilore_status hilore_block_norm_bwd(const hilore_block_norm_bwd_desc *d, int cod
   a.gate_kind = d->gate_kind;
   a.accumulate = accumulate ? 1 : 0;
   a.code = code;
-  for (a.block_log2 = 0; block > (1 << a.block_log2);) ++a.block_log2;
+  // code and block have been checked only if there is an L unit
+  a.block_log2 = (d->h.codes || d->y.codes) && scaled ? __builtin_ctz((unsigned)block) : 0;
   a.sums = sums_over_rows(*d) ? 1 : 0;
   a.groups = hilore::block_norm_bwd_groups(d->rows, d->cols, a.sums);
   a.part = static_cast<float *>(workspace);

@@ -1,0 +1,23 @@
+"""Arguments that hilore_block_norm_bwd does not read: without an L unit its code and block may be
+anything.  Each call runs in a process of its own, so that one that does not return is a failure."""
+import subprocess
+import sys
+
+import pytest
+
+from test_abi import ROOT, lib  # noqa: F401
+
+CALL = """
+import ctypes, sys
+from paper_2609_33570_amd import hilore as E
+d = E.hilore_block_norm_bwd_desc(rows=0, cols=64, scale=1.0)  # nothing to launch
+print(E.load().hilore_block_norm_bwd(ctypes.byref(d), int(sys.argv[1]), int(sys.argv[2]), 0, None, 0, None))
+"""
+
+
+@pytest.mark.parametrize("code,block", [(0, 2 ** 31 - 1), (0, 2 ** 30 + 1), (1, -(2 ** 31)), (-7, -1), (2, 128), (9, 0)])
+def test_code_and_block_of_bf16_units(lib, code, block):  # noqa: F811
+    out = subprocess.run([sys.executable, "-c", CALL, str(code), str(block)], cwd=ROOT, capture_output=True, text=True,
+                         timeout=60)
+    # 5: the runtime's own complaint where there is no device
+    assert out.returncode == 0 and out.stdout.strip() in ("0", "5"), (out.stdout, out.stderr[-500:])
