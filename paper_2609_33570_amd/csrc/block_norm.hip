@@ -561,7 +561,7 @@ int block_norm_bwd_groups(int64_t rows, int64_t cols, int sums) {
 }
 
 hipError_t launch_block_norm_bwd(const BlockNormBwdArgs &a, hipStream_t s) {
-  if (a.cols == 0) return hipSuccess;
+  if (a.cols == 0 || (a.rows == 0 && !a.sums)) return hipSuccess;
   if (a.rows > 0) {
     const bool l = a.h.codes || a.y.codes;
     if (!l) by_pieces<-1, -1>(a, s);

@@ -21,3 +21,9 @@ def test_code_and_block_of_bf16_units(lib, code, block):  # noqa: F811
                          timeout=60)
     # 5: the runtime's own complaint where there is no device
     assert out.returncode == 0 and out.stdout.strip() in ("0", "5"), (out.stdout, out.stderr[-500:])
+
+
+def test_nothing_to_launch(lib):  # noqa: F811
+    """No rows and no sums over rows: HILORE_OK, whatever the runtime has to say (as without a device)."""
+    out = subprocess.run([sys.executable, "-c", CALL, "0", "128"], cwd=ROOT, capture_output=True, text=True, timeout=60)
+    assert out.returncode == 0 and out.stdout.strip() == "0", (out.stdout, out.stderr[-500:])
