@@ -434,7 +434,7 @@ __global__ __launch_bounds__(kThreads, 5) void adamw_kernel(const AdamwBatch a) 
   const int k = __builtin_amdgcn_readfirstlane(tensor_of<128>(a.w, a.cap, blockIdx.x));
   const AdamwTensor t = tensor_at(a, k, clip);
   const int64_t begin = ((int64_t)blockIdx.x - a.w[k]) * kAdamwChunk;
-  if (!(clip <= 1.0f)) return;  // NaN: the step is skipped
+  if (clip != clip) return;  // NaN: the step is skipped
   const Scalars s = {a.beta1, a.one_beta1, a.beta2,
                      a.one_beta2, a.eps, a.inv_sqrt_c2, clip};
   const int param = t.p ? (t.p16 ? 1 : 0) : 2;
