@@ -418,7 +418,9 @@ __global__ __launch_bounds__(kMaxThreads, V == 1 ? 4 : 2) void block_norm_bwd_ke
           s_post[v][2 * k + 1] = fmaf(d.y, p.yh.y, s_post[v][2 * k + 1]);
         }
         d *= p.w;
-        dy[k] = pack_bf16(r_post * fmaf(-c2, p.yh.x, d.x), r_post * fmaf(-c2, p.yh.y, d.y));
+        // not with c2 = 0: a y that is not finite would reach the gradient of a block without norm
+        if (a.w_post) d = f32x2{fmaf(-c2, p.yh.x, d.x), fmaf(-c2, p.yh.y, d.y)};
+        dy[k] = pack_bf16(r_post * d.x, r_post * d.y);
       }
       const int64_t at = row * a.cols + col;
       if (a.dres) store16(a.dres + at, dres);
