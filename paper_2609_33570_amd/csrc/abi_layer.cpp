@@ -469,7 +469,7 @@ hilore_status hilore_adamw(const hilore_adamw_tensor *tensors, int n_tensors, do
   b.has_p = has_p;
   b.has_p16 = has_p16;
   b.stride = 9 + (has_p && has_p16 ? 2 : 0) + (has_scales ? 3 : 0);
-  b.cap = hilore::kAdamwWords / (b.stride + 1);
+  b.cap = hilore::adamw_capacity(b.stride);
   int count;
   clear(b, count);
   // one without elements keeps its number and gets no workgroup

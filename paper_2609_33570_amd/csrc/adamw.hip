@@ -393,9 +393,9 @@ __device__ __forceinline__ T *global_at(uint64_t a) {
 // follows it in the batch).
 __device__ __forceinline__ AdamwTensor tensor_at(const AdamwBatch &a, int k, float clip) {
   const uint32_t *rec = a.w + a.cap + k * a.stride;
-  uint32_t r[16];
+  uint32_t r[kAdamwRecord];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) r[i] = rec[i];
+  for (int i = 0; i < kAdamwRecord; ++i) r[i] = rec[i];
   // all of them in one wait: each load on its own is a trip to the host's memory
   asm volatile("" ::"s"(r[0]), "s"(r[1]), "s"(r[2]), "s"(r[3]), "s"(r[4]), "s"(r[5]), "s"(r[6]), "s"(r[7]),
                "s"(r[8]), "s"(r[9]), "s"(r[10]), "s"(r[11]), "s"(r[12]), "s"(r[13]), "s"(a.w[k]), "s"(a.eps),

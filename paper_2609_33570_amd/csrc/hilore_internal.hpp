@@ -288,7 +288,10 @@ constexpr int64_t kAdamwChunk = 4096;     // elements per workgroup
 //   param  6 param (p, else p16)  7 step size lr / (1 - beta1^step)  8 decay 1 - lr * weight_decay
 //   with both p and p16:  p16 and its upper half;  with 8-bit states:  m_scales, v_scales and
 //   their upper halves
-constexpr int kAdamwWords = 1008;
+constexpr int kAdamwWords = 1008, kAdamwRecord = 14;
+// Tensors of a launch with records of `stride` words: a kernel reads kAdamwRecord words of each,
+// the last one's too, and all of them lie in the words.
+constexpr int adamw_capacity(int stride) { return (kAdamwWords - kAdamwRecord + stride) / (stride + 1); }
 struct AdamwBatch {
   uint32_t w[kAdamwWords];
   const float *norm;
