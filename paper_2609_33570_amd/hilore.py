@@ -217,7 +217,10 @@ def _code(code) -> int:
 def unit_desc(x=None, codes=None, scales=None, xhat=None, row_ss_x=None, row_ss_err=None,
               rows=None, cols=None, ld=None) -> hilore_unit_desc:
     """Descriptor of one unit from torch tensors (shapes taken from the tensors
-    when not given: x is [rows, ld] with ld = row stride; codes [rows, cols])."""
+    when not given: x is [rows, ld] with ld = row stride; codes [rows, cols]).
+    It keeps a reference to what the backward reads of the unit: codes and scales, or x where
+    there are no codes.  What is only encoded from (x beside codes) or written may go once the
+    call that uses it has been made."""
     ref = x if x is not None else (codes if codes is not None else xhat)
     if rows is None:
         rows = ref.shape[0] if ref is not None else (row_ss_x.shape[0] if row_ss_x is not None else 0)
@@ -230,8 +233,10 @@ def unit_desc(x=None, codes=None, scales=None, xhat=None, row_ss_x=None, row_ss_
             cols = x.shape[1]
     if ld is None:
         ld = x.stride(0) if x is not None else cols
-    return hilore_unit_desc(_p_rows(x), _p(codes), _p(scales), _p(xhat), _p(row_ss_x),
+    desc = hilore_unit_desc(_p_rows(x), _p(codes), _p(scales), _p(xhat), _p(row_ss_x),
                             _p(row_ss_err), int(rows), int(cols), int(ld))
+    desc._tensors = (x,) if codes is None else (codes, scales)
+    return desc
 
 
 def _desc_array(units: Sequence[hilore_unit_desc]):
@@ -505,8 +510,8 @@ def hilore_update_sparsity(coeff, flags, adv, mask, R: int, T: int, top_frac: fl
 
 # ------------------------------------------------------------- layer operators --
 # Their descriptors hold the data pointers of the tensors they are made from, and a reference
-# to each (but for those of the unit descriptors given to block_norm_bwd_desc): a trainer makes
-# them once and keeps them from step to step.
+# to each (block_norm_bwd_desc to its units, which keep theirs): a trainer makes them once and
+# keeps them from step to step.
 def _keeping(desc, *tensors):
     desc._tensors = tensors
     return desc
@@ -606,7 +611,7 @@ def block_norm_bwd_desc(h=None, y=None, w_post=None, gate=None, scale: float = 1
                                       _p(gate), _p(w_pre), _p(rstd_post), _p(rstd_pre), _p_rows(dn),
                                       _p(dh), _p(dres), _p(dy), _p(dw_post), _p(dw_pre), _p(dgate),
                                       rows, cols, _rows_of(dn), float(scale), kind)
-    return _keeping(desc, w_post, gate, w_pre, rstd_post, rstd_pre, dn, dh, dres, dy, dw_post,
+    return _keeping(desc, h, y, w_post, gate, w_pre, rstd_post, rstd_pre, dn, dh, dres, dy, dw_post,
                     dw_pre, dgate)
 
 
