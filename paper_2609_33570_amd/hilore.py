@@ -591,6 +591,8 @@ def block_norm_bwd_desc(h=None, y=None, w_post=None, gate=None, scale: float = 1
     else bf16 x), dn (rows may be padded), dh, dres and dy bf16 [rows, cols], dw_* f32 [cols],
     dgate f32 [cols] or [rows, 1], or bf16 [rows, cols], like the gate."""
     ref = dn if dn is not None else dh
+    if ref is None:
+        raise ValueError("a backward needs dn or dh")
     rows, cols = (int(d) for d in ref.shape)
     for t, name in ((dn, "dn"), (dh, "dh"), (dres, "dres"), (dy, "dy")):
         _sized(_typed(t, name, "bfloat16"), name, rows, cols)

@@ -1,5 +1,6 @@
-"""Arguments that hilore_block_norm_bwd does not read: without an L unit its code and block may be
-anything.  Each call runs in a process of its own, so that one that does not return is a failure."""
+"""Arguments of hilore_block_norm_bwd that it does not read, or lacks: without an L unit its code
+and block may be anything.  Each call runs in a process of its own, so that one that does not return
+is a failure."""
 import subprocess
 import sys
 
@@ -27,3 +28,11 @@ def test_nothing_to_launch(lib):  # noqa: F811
     """No rows and no sums over rows: HILORE_OK, whatever the runtime has to say (as without a device)."""
     out = subprocess.run([sys.executable, "-c", CALL, "0", "128"], cwd=ROOT, capture_output=True, text=True, timeout=60)
     assert out.returncode == 0 and out.stdout.strip() == "0", (out.stdout, out.stderr[-500:])
+
+
+def test_a_backward_without_gradients():
+    """Neither dn nor dh: refused by the binding with a message, as by the library."""
+    from paper_2609_33570_amd import hilore as E
+
+    with pytest.raises(ValueError, match="dn or dh"):
+        E.block_norm_bwd_desc()
