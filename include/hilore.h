@@ -566,7 +566,8 @@ hilore_status hilore_block_norm_bwd(const hilore_block_norm_bwd_desc *d, int cod
  * scale per token:
  *   a[t][k] = RNE(x'[t][k] * (127 / amax_t)) clamped to [-127, 127],  sa_t = amax_t / 127,
  *             x' = x * factor (fp32), amax_t = max_k |x'[t][k]|  (IEEE fp32 quotients;
- *             amax_t < 2^-64: codes and sa_t are 0; not finite: codes 0, sa_t NaN)
+ *             amax_t < 2^-64: codes and sa_t are 0; not finite: codes 0, sa_t NaN;
+ *             127 times a reciprocal instead of the quotient moves about one code in a million)
  *   out[t][n] (+)= (sum_k a[t][k] * w[n][k]) * sa_t * sw_n + bias[n]
  * The sums are exact in int32 (k <= 131072); the rest is fp32 in that order, rounded
  * once to the output's type.
@@ -664,7 +665,8 @@ hilore_status hilore_grad_norm(const hilore_adamw_tensor *tensors, int n_tensors
  * One AdamW step (decoupled weight decay) over many tensors, g = grad * norm[1]:
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
  *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
- * fp32 arithmetic; the update uses the new states before their rounding.
+ * fp32 arithmetic; the update uses the new states before their rounding, and its quotient is a
+ * product with a reciprocal within one unit in the last place.
  *   norm     f32 [2] of hilore_grad_norm, or NULL: g = grad.  Where norm[1] is NaN
  *            nothing is written (a step with an infinite or NaN gradient is skipped)
  *   step     1 for the first step
@@ -673,7 +675,8 @@ hilore_status hilore_grad_norm(const hilore_adamw_tensor *tensors, int n_tensors
  * codec's), codes of |value| * (448 * (1/amax)), and a value between two codes takes the upper one with the probability of
  * its place between them, so that the rounding is unbiased and changes far below a
  * code's spacing, as (1 - beta2) makes them, add up over steps instead of vanishing.
- * r > 0 never becomes code 0: a lost second moment would leave eps alone under m.
+ * r > 0 never becomes code 0: a lost second moment would leave eps alone under m.  A gradient
+ * or state that is not finite (in a step that no norm skips) makes its own block so, and no other.
  * Random bits: 32 per element, R = mix(i ^ K), K = mix(seed + 0x9E3779B1 (tensor + 1) + salt)
  * in 32-bit arithmetic with i the element's index (below 2^32) in tensor `tensor` of the
  * call, mix(x): x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xBB67AE85, x ^= x >> 16.

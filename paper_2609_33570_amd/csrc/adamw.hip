@@ -15,7 +15,8 @@
 //
 // Bound by HBM: per element 28 B with everything in fp32 (p, m, v read and
 // written, g read), 10 B with bf16 parameters and gradients and 8-bit states.  The step runs at
-// 5.3 TB/s of those bytes (40M fp32 elements 210 us, 233M with 8-bit states 440), the norm at 4.0.
+// 5.0 to 5.3 TB/s of those bytes (40M fp32 elements 210 us, 233M with 8-bit states 440 to 463, kernel
+// times under a trace on different machines), the norm at 4.0.
 #include "device_common.hpp"
 #include "hilore_internal.hpp"
 
@@ -127,7 +128,8 @@ __device__ __forceinline__ void decode(const Lane<uint8_t, E> &l, float s, float
 
 // Codes of a block's values (E of 256 in each lane) with 16 random bits each, and the block's
 // scale.  KEEP: x >= 0, and what is above zero stays above it.  BIG: blocks up to fp32's
-// largest; else up to 2^12, where 448 / amax 2^-120 is a normal number.
+// largest; else up to 2^12, where 448 / amax 2^-120 is a normal number.  The two differ by a
+// rounding of products below 2^-126, 2^-20 of the least code's spacing.
 template <bool KEEP, bool BIG, int E>
 __device__ __forceinline__ void encode(const float x[E], const uint32_t bits[E], float amax,
                                        Lane<uint8_t, E> &out, float &scale) {
@@ -135,7 +137,7 @@ __device__ __forceinline__ void encode(const float x[E], const uint32_t bits[E],
   float inv;
   if constexpr (BIG) {
     inv = 1.0f / amax;
-  } else {  // one Newton step after the hardware's
+  } else {  // one Newton step after the hardware's: 1 / amax to the bit for every fp32 in [2^-64, 2^12]
     inv = __builtin_amdgcn_rcpf(amax);
     inv = fmaf(fmaf(-amax, inv, 1.0f), inv, inv);
   }
@@ -172,7 +174,8 @@ __device__ __forceinline__ float block_amax(const float x[E]) {
 }
 
 // Roots of v >= 0: a Newton step after the hardware's reciprocal root, which is for normal
-// numbers (the library's sqrtf, three times as long, for the others).
+// numbers (the library's sqrtf, three times as long, for the others).  Over all normal numbers it is
+// sqrtf but for 0.08 %, by one unit in the last place, none of them in [2^-64, 2^13).
 template <int E>
 __device__ __forceinline__ void roots(const float v[E], float r[E]) {
   bool other = false;
@@ -268,7 +271,8 @@ __device__ __forceinline__ void step_piece(Piece<EIGHT, GRAD16, PARAM> &x, const
   }
   roots<E>(v, r);
 #pragma unroll
-  for (int k = 0; k < E; ++k)  // rcp is within 1 ulp; eps keeps its operand a normal number
+  for (int k = 0; k < E; ++k)  // rcp is within 1 ulp of the quotient, of a step that is far below p;
+                               // eps keeps its operand a normal number
     p[k] = p[k] * t.decay -
            (t.step_size * m[k]) * __builtin_amdgcn_rcpf(r[k] * s.inv_sqrt_c2 + s.eps);
   if constexpr (EIGHT) {
@@ -389,8 +393,8 @@ __device__ __forceinline__ T *global_at(uint64_t a) {
   return (T *)(__attribute__((address_space(1))) T *)a;
 }
 
-// Tensor k of a launch; its whole record is read at once (a shorter one with some of what
-// follows it in the batch).
+// Tensor k of a launch; its whole record is read at once (a shorter one with some of the words
+// that follow it).
 __device__ __forceinline__ AdamwTensor tensor_at(const AdamwBatch &a, int k, float clip) {
   const uint32_t *rec = a.w + a.cap + k * a.stride;
   uint32_t r[kAdamwRecord];
@@ -422,11 +426,12 @@ __device__ __forceinline__ AdamwTensor tensor_at(const AdamwBatch &a, int k, flo
   return t;
 }
 
-// Five waves a SIMD, with some spills in the kinds of most operands (a step with its norm: 28
-// adapters in 8 bit 16.3 -> 14.0 us, 233M elements 564 -> 554).  By the tensors' packing into
-// fewer launches, 343 of 215 elements: 85 -> 65 us, 392 adapters of 40M elements 304 -> 268.
 __device__ const float kNoClip[2] = {0.0f, 1.0f};
 
+// One kernel for all kinds, since the tensors of a launch may differ in kind; its registers are
+// those of the kind of most operands.  Bounded to five waves a SIMD, with 20 of them spilled there (a
+// step with its norm: 28 adapters in 8 bit 16.3 -> 14.0 us, 233M elements 564 -> 554).  By the tensors'
+// packing into fewer launches, 343 of 215 elements: 85 -> 65 us, 392 adapters of 40M elements 304 -> 268.
 __global__ __launch_bounds__(kThreads, 5) void adamw_kernel(const AdamwBatch a) {
   // a uniform load, asked for before the tensors' first chunks are there
   const uintptr_t norm = reinterpret_cast<uintptr_t>(a.norm ? a.norm : kNoClip);
@@ -518,8 +523,11 @@ __global__ __launch_bounds__(kFoldThreads) void norm_fold_kernel(const double *p
   for (int64_t i = threadIdx.x; i < n; i += kFoldThreads) sum += part[i];
   sum = group_sum(sum, lds);
   if (threadIdx.x == 0) {
-    // the sum rounded to 24 bits, then fp32 operations (a 53-bit root of 24 bits rounds
-    // to the same fp32 as theirs; fp32's exponents would not hold every sum)
+    // The sum rounded to 24 bits, then fp32 operations (a 53-bit root of 24 bits rounds
+    // to the same fp32 as theirs; fp32's exponents would not hold every sum).  These are the bits that
+    // a trainer's own fp32 root, sum and quotient give on an exact sum, and the random rounding below
+    // 8-bit states turns on single bits of the factor.  The roundings put the factor up to 3
+    // units of 2^-24 from 64 bits (0.6 in the mean); one rounding at the end would put it 1 (0.36).
     const uint64_t u = __builtin_bit_cast(uint64_t, sum);
     const double sum24 =
         __builtin_bit_cast(double, (u + 0xFFFFFFFu + ((u >> 29) & 1u)) & ~uint64_t(0x1FFFFFFF));

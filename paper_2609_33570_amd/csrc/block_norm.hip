@@ -11,8 +11,10 @@
 // columns, `threads` pieces apart, so that each load is 16 bytes a lane and contiguous over
 // the wave.  Workgroups stay for many rows; up to 8192 columns they keep the weights in
 // registers and load the next row before they work on this one, so that neither the loads'
-// latency nor the barriers of the row sums leave the memory idle.  16384 x 3584: forward 100 us,
-// 4.7 TB/s, the rate of a large copy; backward with all gradients 152 us, 4.6 TB/s.
+// latency nor the barriers of the row sums leave the memory idle.  16384 x 3584, whole passes in
+// a row: forward 101 us, 4.7 TB/s, the rate of a large copy; backward with all gradients, its fold
+// included, 152 us, 4.6 TB/s (under a kernel trace 162 to 177 and 5).  Longer rows are loaded when their
+// turn comes: 4096 x 14336 forward 126 us, 3.7 TB/s, backward 212 us, 3.3 TB/s.
 #include "device_common.hpp"
 #include "hilore_internal.hpp"
 
@@ -57,7 +59,8 @@ __device__ __forceinline__ u32x4 load16(const uint16_t *p) {
 
 constexpr uint32_t kOnes = 0x3F803F80u;  // two bf16 ones
 
-// Outputs go past the caches, which the next row's operands need (16384 x 896: 27.0 -> 21.9 us).
+// Outputs go past the caches, which the next row's operands need (16384 x 896: 27.0 -> 21.9 us;
+// not measured for a few rows, whose reader would find them there).
 __device__ __forceinline__ void store16(uint16_t *p, u32x4 v) {
   __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p));
 }

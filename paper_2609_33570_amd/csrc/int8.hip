@@ -318,7 +318,7 @@ __global__ __launch_bounds__(256) void int8_join_kernel(const Int8Args a, int pa
 // position g ^ (r / 4 % 4), which spreads the 16 rows that one cycle of a fragment read takes
 // over all banks.  Four stages are in flight.
 // A large product is bound by the matrix units at the clock their power allows: 16384 x 3584 x 18944
-// takes 1080 us, 2.06 POP/s; the outputs' way through LDS (5 us a tile) is not covered by products.
+// takes 1040 to 1090 us on different machines, 2.04 to 2.15 POP/s; the outputs' way through LDS (5 us a tile) is not covered by products.
 constexpr int kStageK = 64, kTileThreads = 256;
 constexpr int kTurnK = 4 * kStageK;  // a turn of the ring
 constexpr int kGroupT = 16, kBlockT = 8, kBlockN = 4;  // tiles
@@ -681,7 +681,8 @@ __global__ __launch_bounds__(kTileThreads, Tile<B>::kPerCu) void int8_tile_kerne
 hipError_t launch_quantize_tokens(const QuantArgs &a, hipStream_t s) {
   if (a.tokens == 0) return hipSuccess;
   // few tokens: as many threads as there are pieces; many: two pieces a thread (16384 x 3584
-  // with 1 / 2 / 4: 42.5 / 34.5 / 37.4 us, x 8192 with 2 / 4: 68.8 / 75.3; 5.1 to 5.9 TB/s)
+  // with 1 / 2 / 4: 42.5 / 34.5 / 37.4 us, x 8192 with 2 / 4: 68.8 / 75.3; 5.1 to 5.9 TB/s
+  // over operands in turn that no cache holds; 46 us and 3.8 TB/s in front of a product, under a trace)
   const int64_t pieces = (a.k + 7) / 8;
   const int v = a.k > kQuantHeld ? 0
                 : a.tokens < 1024 ? (pieces <= 1024 ? 1 : pieces <= 2048 ? 2 : 4)
