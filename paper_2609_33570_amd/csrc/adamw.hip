@@ -271,7 +271,7 @@ __device__ __forceinline__ void step_piece(Piece<EIGHT, GRAD16, PARAM> &x, const
   }
   roots<E>(v, r);
 #pragma unroll
-  for (int k = 0; k < E; ++k)  // rcp is within 1 ulp of the quotient, of a step that is far below p;
+  for (int k = 0; k < E; ++k)  // rcp is within 1 ulp, 2^-23 of the step that is taken from p;
                                // eps keeps its operand a normal number
     p[k] = p[k] * t.decay -
            (t.step_size * m[k]) * __builtin_amdgcn_rcpf(r[k] * s.inv_sqrt_c2 + s.eps);
