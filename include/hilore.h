@@ -22,6 +22,9 @@
  *   norms on leaving a block and entering the next, and back -> hilore_block_norm, hilore_block_norm_bwd
  *   frozen base weights in int8, forward and input gradient  -> hilore_int8_linear, hilore_int8_matmul
  *   optimizer step on the gradients, and their global norm   -> hilore_adamw, hilore_grad_norm
+ *   heads of queries and keys: norm and rotation, and back   -> hilore_qk_norm_rope, hilore_qk_norm_rope_bwd
+ *   log-probabilities of the chosen tokens, and back         -> hilore_token_logprobs, hilore_token_logprobs_bwd
+ *   the loss with its gradient to each log-probability       -> hilore_policy_loss, hilore_preference_loss
  *
  * Conventions shared by every entry point:
  *   - Every tensor pointer is a DEVICE pointer owned by the caller.  The
@@ -38,8 +41,11 @@
  *   - bf16 tensors are passed as uint16_t* (raw bit patterns).
  *   - Alignment: every tensor pointer must be 16-byte aligned, except the
  *     per-unit outputs of hilore_unit_exposure_risk (4-byte aligned), the
- *     per-unit arrays of hilore_allocate (8-byte aligned for fp64) and the
- *     scales of 8-bit optimizer states (4-byte aligned).
+ *     per-unit arrays of hilore_allocate (8-byte aligned for fp64), the
+ *     scales of 8-bit optimizer states (4-byte aligned) and, with the alignment
+ *     of their elements, positions, inv_freq and all tensors of
+ *     hilore_token_logprobs, its backward and the losses (shifted slices of
+ *     logits, tokens and masks are theirs).
  *   - The functions are re-entrant; calls on different streams may run
  *     concurrently.  No C++ exception crosses this interface.
  *   - Results do not depend on the launch configuration: every reduction is
@@ -692,6 +698,313 @@ hilore_status hilore_grad_norm(const hilore_adamw_tensor *tensors, int n_tensors
 hilore_status hilore_adamw(const hilore_adamw_tensor *tensors, int n_tensors, double beta1,
                            double beta2, double eps, int64_t step, const float *norm,
                            uint32_t seed, void *stream);
+
+/* Which columns of a head are rotated together. */
+typedef enum hilore_rotation {
+  HILORE_ROTATE_HALVES = 0, /* column i with column i + rotated / 2 */
+  HILORE_ROTATE_PAIRS = 1   /* column 2i with column 2i + 1         */
+} hilore_rotation;
+
+/*
+ * From the projections to attention: the norm of every head of the queries and keys
+ * and the rotation by its token's position, in one pass.  For head j of token t, x its
+ * `dim` columns:
+ *   n = x * rsqrt(mean(x^2) + eps) * w      (n = x without w)
+ *   (a, b) -> rope_scale * (a cos - b sin, b cos + a sin)  for the i-th two of the first
+ *   `rotated` columns of n (rotation), angle = position * inv_freq[i]; other columns of n
+ *   as they are
+ *   q, k       bf16 [tokens, heads * dim], row strides ld_q and ld_k (a slice of the joint
+ *              projection's rows); heads_k may be 0 (k fields unused)
+ *   w_q, w_k   bf16 [dim]; NULL: no norm of the queries' / keys' heads
+ *   positions  i64 [tokens]; NULL: t.  A negative position is padding: the token's inputs
+ *              are not read and its outputs are 0
+ *   inv_freq   f32 [rotated / 2]; not read where rotated is 0
+ * Outputs: q_out, k_out bf16, column c of head j of token t at t * token_stride +
+ * j * head_stride + c: [tokens, heads, dim] or [heads, tokens, dim], dense or padded.
+ * q_out may be q where the strides are those of q's rows, k_out k likewise.
+ * fp32 arithmetic with one rounding at the end; angles in pairs of fp64 (whole turns are taken
+ * off before position * inv_freq is rounded: positions up to 2^53 turn as exactly as near ones).
+ * Limits: dim % 16 == 0, dim <= 512, rotated % 16 == 0, rotated <= dim, strides % 8 == 0,
+ * heads_q + heads_k <= 65536, tokens < 2^31.
+ */
+typedef struct hilore_qk_norm_rope_desc {
+  const uint16_t *q;
+  const uint16_t *k;
+  const uint16_t *w_q;
+  const uint16_t *w_k;
+  const int64_t *positions;
+  const float *inv_freq;
+  uint16_t *q_out;
+  uint16_t *k_out;
+  int64_t tokens;
+  int64_t ld_q;
+  int64_t ld_k;
+  int64_t q_token_stride;
+  int64_t q_head_stride;
+  int64_t k_token_stride;
+  int64_t k_head_stride;
+  int heads_q;
+  int heads_k;
+  int dim;
+  int rotated;
+  float eps;
+  float rope_scale;
+  int rotation;
+} hilore_qk_norm_rope_desc;
+hilore_status hilore_qk_norm_rope(const hilore_qk_norm_rope_desc *d, void *stream);
+
+/*
+ * Backward of hilore_qk_norm_rope.  With g the gradient of a head's output, r its
+ * rsqrt factor (formed again from x), means and sums over a head's columns:
+ *   dn = g turned back (by -angle) and times rope_scale,   t = dn * w
+ *   dx = r * (t - x r * mean(t x r))   (dn without w),   dw = sum over tokens and heads of dn x r
+ *   q, k       the saved inputs as units [tokens, heads * dim]: codes (+ scales) for an L
+ *              unit, decoded in registers to the bf16 value hilore_decompress writes,
+ *              otherwise x, bf16 with row stride ld.  Read only with w_q / w_k; either may
+ *              be L (then with the same code and block, heads * dim % block == 0)
+ *   dq, dk     bf16, addressed like the forward's outputs; strides may be 0 (one gradient
+ *              for all tokens or heads)
+ * Outputs: dq_in, dk_in bf16 [tokens, heads * dim], row strides ld_dq and ld_dk (a slice of
+ * the projection's gradient); dq_in may be dq where the strides agree; NULL: not wanted.
+ * dw_q, dw_k f32 [dim] or NULL; accumulate != 0 adds to what is there.
+ * Tokens with a negative position get 0 and give dw nothing (their rows are not read).
+ * workspace: device memory of at least hilore_qk_norm_rope_bwd_workspace_bytes(d) bytes (0, and
+ * then NULL is allowed, without dw), 16-byte aligned, contents on entry irrelevant; calls
+ * sharing it must not overlap.  Sums over tokens and heads in a fixed order.
+ */
+typedef struct hilore_qk_norm_rope_bwd_desc {
+  hilore_unit_desc q;
+  hilore_unit_desc k;
+  const uint16_t *w_q;
+  const uint16_t *w_k;
+  const int64_t *positions;
+  const float *inv_freq;
+  const uint16_t *dq;
+  const uint16_t *dk;
+  uint16_t *dq_in;
+  uint16_t *dk_in;
+  float *dw_q;
+  float *dw_k;
+  int64_t tokens;
+  int64_t q_token_stride;
+  int64_t q_head_stride;
+  int64_t k_token_stride;
+  int64_t k_head_stride;
+  int64_t ld_dq;
+  int64_t ld_dk;
+  int heads_q;
+  int heads_k;
+  int dim;
+  int rotated;
+  float eps;
+  float rope_scale;
+  int rotation;
+} hilore_qk_norm_rope_bwd_desc;
+size_t hilore_qk_norm_rope_bwd_workspace_bytes(const hilore_qk_norm_rope_bwd_desc *d);
+hilore_status hilore_qk_norm_rope_bwd(const hilore_qk_norm_rope_bwd_desc *d, int code, int block,
+                                      int accumulate, void *workspace, size_t workspace_bytes,
+                                      void *stream);
+
+/*
+ * Log-probabilities of chosen tokens, from logits z (the s_t of the update coefficient,
+ * Sec. 3.2).  For a row with target t, over its `vocab` columns:
+ *   m = max z,   S = sum exp(scale (z - m)),   logp = scale (z_t - m) - log S
+ *   entropy = log S - sum p scale (z - m),   p = exp(scale (z - m)) / S
+ *   logits   bf16 or (logits_f32 != 0) f32 [rows, vocab], row stride ld (>= vocab, any
+ *            value: rows may begin anywhere)
+ *   targets  i64 [rows].  A negative target is a row without a token: it is not read and
+ *            its outputs are 0.  A target >= vocab gives logp NaN
+ *   scale    1 / temperature, positive
+ * Outputs f32 [rows], each may be NULL: logp, entropy, row_max = m and log_sum = log S
+ * (which the backward takes: m and log S apart keep what their sum would round away).
+ * Columns of -inf have p = 0; a row of nothing else, or with +inf or NaN, gives NaN.
+ * fp32 arithmetic.  S is summed without the chosen token's own term, which is added last: where
+ * it is nearly all of S, logp = -log1p(the rest) keeps its relative precision.  A
+ * row's bits do not depend on the other rows of the call.
+ * workspace: device memory of at least hilore_token_logprobs_workspace_bytes(d) bytes (few
+ * rows are split over workgroups; 0, and then NULL is allowed, for many), 16-byte aligned,
+ * contents on entry irrelevant; calls sharing it must not overlap.
+ * Limits: rows < 2^31, vocab < 2^28; vocab = 0 only with rows = 0.
+ */
+typedef struct hilore_token_logprobs_desc {
+  const void *logits;
+  const int64_t *targets;
+  float *logp;
+  float *entropy;
+  float *row_max;
+  float *log_sum;
+  int64_t rows;
+  int64_t vocab;
+  int64_t ld;
+  float scale;
+  int logits_f32;
+} hilore_token_logprobs_desc;
+size_t hilore_token_logprobs_workspace_bytes(const hilore_token_logprobs_desc *d);
+hilore_status hilore_token_logprobs(const hilore_token_logprobs_desc *d, void *workspace,
+                                    size_t workspace_bytes, void *stream);
+
+/*
+ * Backward of hilore_token_logprobs, with l_j = scale (z_j - m) - log S and p_j = exp(l_j):
+ *   dz_j = scale (dlogp (1[j = t] - p_j) - dentropy p_j (l_j + entropy))
+ *   row_max, log_sum, entropy   as the forward wrote them (entropy only with dentropy)
+ *   dlogp f32 [rows], dentropy f32 [rows] or NULL
+ *   dlogits  of the logits' type [rows, vocab], row stride ld_out (>= vocab, any value);
+ *            may be the logits themselves where the strides agree
+ * Rows with a negative target, or with dlogp and dentropy both 0 (padding, clipped tokens
+ * and responses without advantage), are not read: their gradient is 0.  A target >= vocab
+ * gives a row of NaN.  Limits as for hilore_token_logprobs.
+ */
+typedef struct hilore_token_logprobs_bwd_desc {
+  const void *logits;
+  const int64_t *targets;
+  const float *row_max;
+  const float *log_sum;
+  const float *entropy;
+  const float *dlogp;
+  const float *dentropy;
+  void *dlogits;
+  int64_t rows;
+  int64_t vocab;
+  int64_t ld;
+  int64_t ld_out;
+  float scale;
+  int logits_f32;
+} hilore_token_logprobs_bwd_desc;
+hilore_status hilore_token_logprobs_bwd(const hilore_token_logprobs_bwd_desc *d, void *stream);
+
+typedef enum hilore_ratio {
+  HILORE_RATIO_TOKEN = 0,   /* exp(s_t - s_t^old) of each token                         */
+  HILORE_RATIO_SEQUENCE = 1 /* exp of the mean of s - s^old over a sequence's valid tokens */
+} hilore_ratio;
+typedef enum hilore_kl {
+  HILORE_KL_NONE = 0,
+  HILORE_KL_K1 = 1, /* x = s - s_ref       */
+  HILORE_KL_K2 = 2, /* x^2 / 2             */
+  HILORE_KL_K3 = 3  /* exp(-x) - 1 + x     */
+} hilore_kl;
+typedef enum hilore_mean {
+  HILORE_MEAN_TOKENS = 0,   /* weight of a valid token: 1 / N                            */
+  HILORE_MEAN_SEQUENCES = 1 /* 1 / (N n_i), n_i the valid tokens of its sequence          */
+} hilore_mean;
+
+/*
+ * Clipped policy loss with a KL term and an entropy bonus (Sec. 3.1 Eq. grpo-objective and
+ * its usual variants): its value, its statistics and its gradient to each log-probability
+ * and entropy.  For a valid token with advantage A and log ratio delta:
+ *   chi    = delta <= log1p(clip_high) where A >= 0, else delta >= log1p(-clip_low)
+ *            (thresholds rounded to fp32, as in hilore_grpo_coeffs) and, with dual_clip > 0
+ *            and A < 0, delta <= log(dual_clip); dual_clip is 0 or above 1
+ *   policy = -A r where chi holds, r = exp(delta), else -A times the bound that delta is past
+ *            (1 + clip_high, 1 - clip_low or dual_clip); 0 where A = 0
+ *   loss   = sum over valid tokens of weight * (policy + beta * kl - entropy_weight * entropy)
+ *   dlogp  = weight * (-chi A r + beta * dkl/ds),   dentropy = -entropy_weight * weight
+ *            (with HILORE_RATIO_SEQUENCE too: the ratio moves by 1 / n_i with each token, and
+ *            the n_i tokens of the sequence share it)
+ * Sequences: rows of equal length n_tokens / sequences one after another, or with
+ * offsets i64 [sequences + 1] (nondecreasing, within [0, n_tokens]) sequence i is the
+ * tokens [offsets[i], offsets[i + 1]), possibly none.  Tokens of no sequence are neither
+ * read nor written.
+ *   logp, logp_old, logp_ref, entropy  f32 [n_tokens]; logp_ref only (and always) with a kl,
+ *            entropy NULL: no bonus (entropy_weight 0, dentropy NULL)
+ *   adv      f32 [sequences], or (adv_per_token != 0) [n_tokens], then with HILORE_RATIO_TOKEN
+ *   mask     u8 [n_tokens] (nonzero = valid), NULL: all.  What is masked is not used, be it
+ *            infinite or NaN
+ *   n_norm   N: > 0 uses this value (of the complete batch); else the number of valid tokens
+ *            (HILORE_MEAN_TOKENS) or of sequences that have any (HILORE_MEAN_SEQUENCES) of
+ *            this call.  Without a valid token loss and gradients are 0
+ * Outputs, each may be NULL: dlogp, dentropy, token_loss (a token's part of the loss) f32
+ * [n_tokens], 0 where masked; flags u8 [n_tokens]: bit 0 valid and chi, bit 1 valid, A != 0
+ * and not chi; stats f32 [8]: loss, weighted sums of policy, kl and entropy, share of the
+ * valid tokens with flag bit 1, their mean ratio, their number, the sequences that have any.
+ * Per-token arithmetic in fp32, sums over tokens in fp64 in a fixed order.
+ * workspace: device memory of at least hilore_policy_loss_workspace_bytes(d) bytes, 16-byte
+ * aligned, contents on entry irrelevant; calls sharing it must not overlap.
+ * Limits: n_tokens < 2^31, sequences < 2^31.
+ */
+typedef struct hilore_policy_loss_desc {
+  const float *logp;
+  const float *logp_old;
+  const float *logp_ref;
+  const float *entropy;
+  const float *adv;
+  const uint8_t *mask;
+  const int64_t *offsets;
+  float *dlogp;
+  float *dentropy;
+  float *token_loss;
+  uint8_t *flags;
+  float *stats;
+  int64_t n_tokens;
+  int64_t sequences;
+  double n_norm;
+  float clip_low;
+  float clip_high;
+  float dual_clip;
+  float beta;
+  float entropy_weight;
+  int adv_per_token;
+  int ratio;
+  int kl;
+  int mean;
+} hilore_policy_loss_desc;
+size_t hilore_policy_loss_workspace_bytes(const hilore_policy_loss_desc *d);
+hilore_status hilore_policy_loss(const hilore_policy_loss_desc *d, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+
+typedef enum hilore_preference {
+  HILORE_PREFERENCE_LOGISTIC = 0, /* (1 - e) softplus(-beta h) + e softplus(beta h), e = label_smoothing */
+  HILORE_PREFERENCE_HINGE = 1,    /* max(0, 1 - beta h)      */
+  HILORE_PREFERENCE_SQUARED = 2   /* (h - 1 / (2 beta))^2    */
+} hilore_preference;
+
+/*
+ * Preference loss over pairs of sequences: its value, statistics and its gradient to each
+ * log-probability.  With L_i the sum (length_mean != 0: the mean) over the valid tokens of
+ * sequence i of logp - logp_ref (logp alone without logp_ref), and h = L_chosen - L_rejected -
+ * margin of a pair:
+ *   loss = (1 / N) sum over pairs of loss(h);   dlogp of a valid token of sequence i =
+ *   (1 / N) (sum of loss'(h) over pairs that choose i - sum over pairs that reject i),
+ *   over n_i with length_mean
+ * Sequences, mask and n_tokens as for hilore_policy_loss.
+ *   chosen, rejected  i32 [pairs] sequence numbers, or both NULL: pair p is sequences 2p and
+ *            2p + 1 (pairs = sequences / 2).  A sequence may be in many pairs, or in none
+ *   n_norm   N: > 0 uses this value; else the number of pairs that take part.  A pair takes
+ *            no part where a number is negative or one of its sequences has no valid token; a
+ *            number >= sequences makes the pair's loss, the statistics and all gradients NaN
+ * Outputs, each may be NULL: dlogp f32 [n_tokens], 0 where masked; rewards f32 [sequences] =
+ * beta L_i; pair_loss f32 [pairs], 0 for a pair that takes no part; stats f32 [6]: loss, and over the pairs that
+ * take part (divided by N) the share with h > 0, the sums of beta h and of the
+ * rewards of the chosen and of the rejected, then the number of pairs that take part.
+ * Token differences in fp32, sums in fp64 in a fixed order.
+ * workspace: device memory of at least hilore_preference_loss_workspace_bytes(d) bytes,
+ * 16-byte aligned, contents on entry irrelevant; calls sharing it must not overlap.
+ * Limits: n_tokens, sequences, pairs < 2^31; with lists sequences * pairs <= 2^36 (each
+ * sequence finds its pairs by reading them).
+ */
+typedef struct hilore_preference_loss_desc {
+  const float *logp;
+  const float *logp_ref;
+  const uint8_t *mask;
+  const int64_t *offsets;
+  const int32_t *chosen;
+  const int32_t *rejected;
+  float *dlogp;
+  float *rewards;
+  float *pair_loss;
+  float *stats;
+  int64_t n_tokens;
+  int64_t sequences;
+  int64_t pairs;
+  double n_norm;
+  float beta;
+  float label_smoothing;
+  float margin;
+  int loss;
+  int length_mean;
+} hilore_preference_loss_desc;
+size_t hilore_preference_loss_workspace_bytes(const hilore_preference_loss_desc *d);
+hilore_status hilore_preference_loss(const hilore_preference_loss_desc *d, void *workspace,
+                                     size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -383,4 +383,92 @@ constexpr int64_t kInt8MaxOut = int64_t(1) << 40;  // tokens * n: tiles are coun
 size_t int8_part_bytes(int64_t tokens, int64_t k, int64_t n);
 hipError_t launch_int8(const Int8Args &a, hipStream_t s);
 
+// Heads of queries and keys: norm and rotation.  One side is the queries or the keys.
+constexpr int kHeadMaxDim = 512;
+struct HeadSide {
+  SavedRows in;              // forward: x alone; backward: read with w
+  const uint16_t *w;         // NULL: no norm
+  const uint16_t *g;         // backward: gradient of the outputs
+  uint16_t *out;             // forward: outputs; backward: gradient of the inputs, or NULL
+  int64_t token_stride, head_stride;  // of the outputs / their gradient
+  int64_t ld_out;            // backward: row stride of out
+  float *dw;
+};
+struct HeadsArgs {
+  HeadSide q, k;
+  const int64_t *positions;
+  const float *inv_freq;
+  int64_t tokens;
+  int heads_q, heads_k, dim, rotated;
+  float eps, inv_dim, rope_scale;
+  int pairs, accumulate;
+  int code, block_log2;
+  int groups;                // backward with dw: workgroups, each with a row of partial sums
+  float *part;               // [q, k][group][dim]
+};
+int heads_bwd_groups(int64_t tokens, int heads, int dim);
+hipError_t launch_heads(const HeadsArgs &a, hipStream_t s);
+hipError_t launch_heads_bwd(const HeadsArgs &a, hipStream_t s);
+
+// Log-probabilities of chosen tokens.
+struct LogprobsArgs {
+  const void *logits;
+  const int64_t *targets;
+  float *logp, *entropy, *row_max, *log_sum;
+  int64_t rows, vocab, ld;
+  float scale;
+  int f32;
+  int split;    // a workgroup a segment, partials to the workspace
+  float *part;  // [row][segment][wave][4]
+};
+size_t logprobs_part_bytes(int64_t rows, int64_t vocab, int f32);
+hipError_t launch_logprobs(const LogprobsArgs &a, hipStream_t s);
+struct LogprobsBwdArgs {
+  const void *logits;
+  const int64_t *targets;
+  const float *row_max, *log_sum, *entropy, *dlogp, *dentropy;
+  void *dlogits;
+  int64_t rows, vocab, ld, ld_out;
+  float scale;
+  int f32;
+};
+hipError_t launch_logprobs_bwd(const LogprobsBwdArgs &a, hipStream_t s);
+
+// Losses.
+struct SequencesArgs {       // sequences of tokens: equal lengths, or offsets
+  const int64_t *offsets;
+  const uint8_t *mask;
+  int64_t tokens, sequences, length;
+};
+struct PolicyArgs {
+  SequencesArgs seq;
+  const float *logp, *old, *ref, *entropy, *adv;
+  float *dlogp, *dentropy, *token_loss, *stats;
+  uint8_t *flags;
+  double n_norm;
+  float bound_high, bound_low, log_high, log_low, dual, log_dual;
+  float beta, bonus;
+  int adv_per_token, sequence_ratio, kl, sequence_mean;
+  uint32_t *count;           // workspace: valid tokens of each sequence
+  float *mean_delta;         // and their mean log ratio
+  double *part;              // partial sums
+};
+size_t policy_workspace(PolicyArgs &a, void *base);
+hipError_t launch_policy(const PolicyArgs &a, hipStream_t s);
+struct PreferenceArgs {
+  SequencesArgs seq;
+  const float *logp, *ref;
+  const int32_t *chosen, *rejected;
+  float *dlogp, *rewards, *pair_loss, *stats;
+  int64_t pairs;
+  double n_norm;
+  float beta, smoothing, margin;
+  int loss, length_mean;
+  uint32_t *count;           // workspace, by sequence
+  double *value, *slope;
+  double *part;
+};
+size_t preference_workspace(PreferenceArgs &a, void *base);
+hipError_t launch_preference(const PreferenceArgs &a, hipStream_t s);
+
 }  // namespace hilore

@@ -92,6 +92,55 @@ class hilore_adamw_tensor(ctypes.Structure):
                    ("grad_bf16", ctypes.c_int)])
 
 
+class hilore_qk_norm_rope_desc(ctypes.Structure):
+    _fields_ = (_pointers("q", "k", "w_q", "w_k", "positions", "inv_freq", "q_out", "k_out")
+                + _int64s("tokens", "ld_q", "ld_k", "q_token_stride", "q_head_stride",
+                          "k_token_stride", "k_head_stride")
+                + [("heads_q", ctypes.c_int), ("heads_k", ctypes.c_int), ("dim", ctypes.c_int),
+                   ("rotated", ctypes.c_int), ("eps", ctypes.c_float),
+                   ("rope_scale", ctypes.c_float), ("rotation", ctypes.c_int)])
+
+
+class hilore_qk_norm_rope_bwd_desc(ctypes.Structure):
+    _fields_ = ([("q", hilore_unit_desc), ("k", hilore_unit_desc)]
+                + _pointers("w_q", "w_k", "positions", "inv_freq", "dq", "dk", "dq_in", "dk_in",
+                            "dw_q", "dw_k")
+                + _int64s("tokens", "q_token_stride", "q_head_stride", "k_token_stride",
+                          "k_head_stride", "ld_dq", "ld_dk")
+                + [("heads_q", ctypes.c_int), ("heads_k", ctypes.c_int), ("dim", ctypes.c_int),
+                   ("rotated", ctypes.c_int), ("eps", ctypes.c_float),
+                   ("rope_scale", ctypes.c_float), ("rotation", ctypes.c_int)])
+
+
+class hilore_token_logprobs_desc(ctypes.Structure):
+    _fields_ = (_pointers("logits", "targets", "logp", "entropy", "row_max", "log_sum")
+                + _int64s("rows", "vocab", "ld")
+                + [("scale", ctypes.c_float), ("logits_f32", ctypes.c_int)])
+
+
+class hilore_token_logprobs_bwd_desc(ctypes.Structure):
+    _fields_ = (_pointers("logits", "targets", "row_max", "log_sum", "entropy", "dlogp", "dentropy",
+                          "dlogits") + _int64s("rows", "vocab", "ld", "ld_out")
+                + [("scale", ctypes.c_float), ("logits_f32", ctypes.c_int)])
+
+
+class hilore_policy_loss_desc(ctypes.Structure):
+    _fields_ = (_pointers("logp", "logp_old", "logp_ref", "entropy", "adv", "mask", "offsets", "dlogp",
+                          "dentropy", "token_loss", "flags", "stats")
+                + _int64s("n_tokens", "sequences") + [("n_norm", ctypes.c_double)]
+                + [(n, ctypes.c_float) for n in ("clip_low", "clip_high", "dual_clip", "beta",
+                                                 "entropy_weight")]
+                + [(n, ctypes.c_int) for n in ("adv_per_token", "ratio", "kl", "mean")])
+
+
+class hilore_preference_loss_desc(ctypes.Structure):
+    _fields_ = (_pointers("logp", "logp_ref", "mask", "offsets", "chosen", "rejected", "dlogp",
+                          "rewards", "pair_loss", "stats")
+                + _int64s("n_tokens", "sequences", "pairs") + [("n_norm", ctypes.c_double)]
+                + [(n, ctypes.c_float) for n in ("beta", "label_smoothing", "margin")]
+                + [("loss", ctypes.c_int), ("length_mean", ctypes.c_int)])
+
+
 _lib = None
 
 
@@ -146,6 +195,16 @@ def load() -> ctypes.CDLL:
         "hilore_grad_norm_workspace_bytes": (ctypes.c_size_t, [P, i32]),
         "hilore_grad_norm": (i32, [P, i32, f64, P, P, ctypes.c_size_t, P]),
         "hilore_adamw": (i32, [P, i32, f64, f64, f64, i64, P, ctypes.c_uint32, P]),
+        "hilore_qk_norm_rope": (i32, [P, P]),
+        "hilore_qk_norm_rope_bwd_workspace_bytes": (ctypes.c_size_t, [P]),
+        "hilore_qk_norm_rope_bwd": (i32, [P, i32, i32, i32, P, ctypes.c_size_t, P]),
+        "hilore_token_logprobs_workspace_bytes": (ctypes.c_size_t, [P]),
+        "hilore_token_logprobs": (i32, [P, P, ctypes.c_size_t, P]),
+        "hilore_token_logprobs_bwd": (i32, [P, P]),
+        "hilore_policy_loss_workspace_bytes": (ctypes.c_size_t, [P]),
+        "hilore_policy_loss": (i32, [P, P, ctypes.c_size_t, P]),
+        "hilore_preference_loss_workspace_bytes": (ctypes.c_size_t, [P]),
+        "hilore_preference_loss": (i32, [P, P, ctypes.c_size_t, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -758,3 +817,321 @@ def hilore_adamw(tensors, beta1: float, beta2: float, eps: float, step: int, nor
            load().hilore_adamw(arr, len(arr), float(beta1), float(beta2), float(eps), int(step),
                                _p(_typed(norm, "norm", "float32")), int(seed) & 0xFFFFFFFF,
                                _stream(stream)))
+
+
+# ------------------------------------------- heads, log-probabilities, losses --
+def _on_device(desc, *tensors):
+    """desc, keeping its tensors, which must all be on one device: the calls refuse another."""
+    found = {t.device.index for t in tensors if t is not None}
+    if len(found) > 1:
+        raise ValueError(f"tensors on several devices: {sorted(map(str, found))}")
+    desc._device = found.pop() if found else None
+    return _keeping(desc, *tensors)
+
+
+def _current(desc):
+    """The descriptor's address, refused where its tensors are not on the current device (whose
+    stream and memory the call uses)."""
+    device = getattr(desc, "_device", None)
+    if device is not None:
+        import torch
+
+        if device != torch.cuda.current_device():
+            raise ValueError(f"tensors on device {device}, the current one is "
+                             f"{torch.cuda.current_device()}")
+    return ctypes.byref(desc)
+
+
+ROTATIONS = {"halves": 0, "pairs": 1}
+RATIOS = {"token": 0, "sequence": 1}
+MEANS = {"tokens": 0, "sequences": 1}
+PREFERENCES = {"logistic": 0, "hinge": 1, "squared": 2}
+
+
+def _choice(value, names, name: str) -> int:
+    if isinstance(value, str):
+        if value not in names:
+            raise ValueError(f"{name} must be one of {sorted(names)}, got {value!r}")
+        return names[value]
+    return int(value)
+
+
+def _heads_of(t, name: str):
+    """(pointer, tokens, heads, dim, token stride, head stride) of bf16 [tokens, heads, dim]; the
+    stride of an axis of one says nothing."""
+    if t is None:
+        return None, 0, 0, 0, 0, 0
+    _device(_typed(t, name, "bfloat16"))
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be [tokens, heads, dim] with contiguous columns, got shape "
+                         f"{tuple(t.shape)}, strides {tuple(t.stride())}")
+    tokens, heads, dim = (int(d) for d in t.shape)
+    by_head = t.stride(1) if heads > 1 else dim
+    by_token = t.stride(0) if tokens > 1 else heads * dim
+    return t.data_ptr(), tokens, heads, dim, by_token, by_head
+
+
+def _head_rows(t, name: str, tokens: int, heads: int, dim: int):
+    """(pointer, row stride) of bf16 [tokens, heads * dim] or [tokens, heads, dim], whose heads lie
+    side by side in rows that may be padded."""
+    if t is None:
+        return None, 0
+    _typed(t, name, "bfloat16")
+    if t.dim() == 3:
+        _sized(t, name, tokens, heads, dim)
+        _device(t)
+        if (dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim):
+            raise ValueError(f"the heads of {name} must lie side by side, got strides {tuple(t.stride())}")
+        return t.data_ptr(), t.stride(0) if tokens > 1 else heads * dim
+    _sized(t, name, tokens, heads * dim)
+    return _p_rows(t), t.stride(0) if tokens > 1 else heads * dim
+
+
+def _same_heads(q, k):
+    if k[0] is not None and (k[1] != q[1] or k[3] != q[3]):
+        raise ValueError(f"queries of {q[1]} tokens and dim {q[3]}, keys of {k[1]} and {k[3]}")
+
+
+def _rotated(inv_freq) -> int:
+    return 0 if inv_freq is None else 2 * int(_typed(inv_freq, "inv_freq", "float32").numel())
+
+
+def qk_norm_rope_desc(q, q_out, k=None, k_out=None, inv_freq=None, positions=None, w_q=None,
+                      w_k=None, eps: float = 1e-6, rope_scale: float = 1.0,
+                      rotation="halves") -> hilore_qk_norm_rope_desc:
+    """Descriptor of hilore_qk_norm_rope: q and k bf16 [tokens, heads * dim] (or [tokens, heads,
+    dim]; rows may be padded, as slices of a joint projection are), outputs bf16 [tokens, heads,
+    dim] of any strides (a transposed [heads, tokens, dim] too), weights bf16 [dim], inv_freq f32
+    [rotated / 2] (None: no rotation), positions i64 [tokens] (None: 0, 1, ...; negative: padding)."""
+    qo, ko = _heads_of(q_out, "q_out"), _heads_of(k_out, "k_out")
+    if q is None or q_out is None or (k is None) != (k_out is None):
+        raise ValueError("queries and keys need an input and an output each")
+    _same_heads(qo, ko)
+    tokens, dim = qo[1], qo[3]
+    qp, ld_q = _head_rows(q, "q", tokens, qo[2], dim)
+    kp, ld_k = _head_rows(k, "k", tokens, ko[2], dim)
+    for t, name in ((w_q, "w_q"), (w_k, "w_k")):
+        _sized(_typed(t, name, "bfloat16"), name, dim)
+    _sized(_typed(positions, "positions", "int64"), "positions", tokens)
+    desc = hilore_qk_norm_rope_desc(qp, kp, _p(w_q), _p(w_k), _p(positions), _p(inv_freq), qo[0], ko[0],
+                                    tokens, ld_q, ld_k, qo[4], qo[5], ko[4], ko[5], qo[2], ko[2], dim,
+                                    _rotated(inv_freq), float(eps), float(rope_scale),
+                                    _choice(rotation, ROTATIONS, "rotation"))
+    return _on_device(desc, q, k, w_q, w_k, positions, inv_freq, q_out, k_out)
+
+
+def hilore_qk_norm_rope(desc: hilore_qk_norm_rope_desc, stream=None):
+    """q_out, k_out = the heads of q and k normed and rotated by their tokens' positions."""
+    _check("hilore_qk_norm_rope", load().hilore_qk_norm_rope(_current(desc), _stream(stream)))
+
+
+def qk_norm_rope_bwd_desc(dq, dk=None, dq_in=None, dk_in=None, q=None, k=None, inv_freq=None,
+                          positions=None, w_q=None, w_k=None, dw_q=None, dw_k=None, eps: float = 1e-6,
+                          rope_scale: float = 1.0, rotation="halves") -> hilore_qk_norm_rope_bwd_desc:
+    """Descriptor of hilore_qk_norm_rope_bwd: dq and dk bf16 [tokens, heads, dim] of any strides,
+    dq_in and dk_in bf16 [tokens, heads * dim] (or [tokens, heads, dim]; rows may be padded), q and k
+    the saved inputs as unit descriptors [tokens, heads * dim] (needed with w_q / w_k), dw_* f32
+    [dim]; the rest as in the forward."""
+    if dq is None:
+        raise ValueError("a backward needs dq")
+    qg, kg = _heads_of(dq, "dq"), _heads_of(dk, "dk")
+    _same_heads(qg, kg)
+    tokens, dim = qg[1], qg[3]
+    qp, ld_q = _head_rows(dq_in, "dq_in", tokens, qg[2], dim)
+    kp, ld_k = _head_rows(dk_in, "dk_in", tokens, kg[2], dim)
+    if dk is None and (dk_in is not None or dw_k is not None):
+        raise ValueError("gradients of keys without dk")
+    for t, name in ((w_q, "w_q"), (w_k, "w_k")):
+        _sized(_typed(t, name, "bfloat16"), name, dim)
+    for t, name in ((dw_q, "dw_q"), (dw_k, "dw_k")):
+        _sized(_typed(t, name, "float32"), name, dim)
+    _sized(_typed(positions, "positions", "int64"), "positions", tokens)
+    none = hilore_unit_desc()
+    desc = hilore_qk_norm_rope_bwd_desc(none if q is None else q, none if k is None else k, _p(w_q),
+                                        _p(w_k), _p(positions), _p(inv_freq), qg[0], kg[0], qp, kp,
+                                        _p(dw_q), _p(dw_k), tokens, qg[4], qg[5], kg[4], kg[5], ld_q,
+                                        ld_k, qg[2], kg[2], dim, _rotated(inv_freq), float(eps),
+                                        float(rope_scale), _choice(rotation, ROTATIONS, "rotation"))
+    saved = [t for u in (q, k) if u is not None for t in getattr(u, "_tensors", ())]
+    return _on_device(desc, w_q, w_k, positions, inv_freq, dq, dk, dq_in, dk_in, dw_q, dw_k, *saved)
+
+
+def hilore_qk_norm_rope_bwd_workspace_bytes(desc: hilore_qk_norm_rope_bwd_desc) -> int:
+    return int(load().hilore_qk_norm_rope_bwd_workspace_bytes(ctypes.byref(desc)))
+
+
+def hilore_qk_norm_rope_bwd(desc: hilore_qk_norm_rope_bwd_desc, code=0, block: int = 0,
+                            accumulate: bool = False, workspace=None, stream=None):
+    """Gradients of hilore_qk_norm_rope.  code and block are those of the L units among q and k (not
+    read without one).  workspace: a device tensor of at least
+    hilore_qk_norm_rope_bwd_workspace_bytes(desc) bytes, or None (taken from torch's allocator)."""
+    address = _current(desc)
+    need = hilore_qk_norm_rope_bwd_workspace_bytes(desc) if workspace is None else 0
+    wp, wb, _keep = _workspace(workspace, need, stream)
+    _check("hilore_qk_norm_rope_bwd",
+           load().hilore_qk_norm_rope_bwd(address, _code(code), int(block), 1 if accumulate else 0, wp,
+                                          wb, _stream(stream)))
+
+
+def _logits_of(t, name: str, rows: int, vocab: int):
+    """(pointer, row stride) of bf16 or f32 logits; rows may be padded and begin anywhere."""
+    _sized(_typed(t, name, "bfloat16", "float32"), name, rows, vocab)
+    return _p_rows(t), t.stride(0) if rows > 1 else vocab
+
+
+def _per_row(rows: int, **tensors):
+    for name, t in tensors.items():
+        _sized(_typed(t, name, "float32"), name, rows)
+
+
+def token_logprobs_desc(logits, targets, logp=None, entropy=None, row_max=None, log_sum=None,
+                        scale: float = 1.0) -> hilore_token_logprobs_desc:
+    """Descriptor of hilore_token_logprobs: logits bf16 or f32 [rows, vocab] (rows may be padded),
+    targets i64 [rows] (negative: a row without a token), outputs f32 [rows]; scale is the
+    inverse temperature."""
+    rows, vocab = (int(d) for d in logits.shape)
+    lp, ld = _logits_of(logits, "logits", rows, vocab)
+    _sized(_typed(targets, "targets", "int64"), "targets", rows)
+    _per_row(rows, logp=logp, entropy=entropy, row_max=row_max, log_sum=log_sum)
+    desc = hilore_token_logprobs_desc(lp, _p(targets), _p(logp), _p(entropy), _p(row_max), _p(log_sum),
+                                      rows, vocab, ld, float(scale), 0 if logits.element_size() == 2 else 1)
+    return _on_device(desc, logits, targets, logp, entropy, row_max, log_sum)
+
+
+def hilore_token_logprobs_workspace_bytes(desc: hilore_token_logprobs_desc) -> int:
+    return int(load().hilore_token_logprobs_workspace_bytes(ctypes.byref(desc)))
+
+
+def hilore_token_logprobs(desc: hilore_token_logprobs_desc, workspace=None, stream=None):
+    """Log-probabilities of the targets, entropies, maxima and log sums of the rows.  workspace: a
+    device tensor of at least hilore_token_logprobs_workspace_bytes(desc) bytes, or None (taken from
+    torch's allocator)."""
+    address = _current(desc)
+    need = hilore_token_logprobs_workspace_bytes(desc) if workspace is None else 0
+    wp, wb, _keep = _workspace(workspace, need, stream)
+    _check("hilore_token_logprobs", load().hilore_token_logprobs(address, wp, wb, _stream(stream)))
+
+
+def token_logprobs_bwd_desc(logits, targets, row_max, log_sum, dlogp, dlogits, entropy=None,
+                            dentropy=None, scale: float = 1.0) -> hilore_token_logprobs_bwd_desc:
+    """Descriptor of hilore_token_logprobs_bwd: row_max, log_sum (and entropy, with dentropy) as the
+    forward wrote them, dlogp and dentropy f32 [rows], dlogits of the logits' type [rows, vocab]
+    (rows may be padded; may be the logits)."""
+    rows, vocab = (int(d) for d in logits.shape)
+    lp, ld = _logits_of(logits, "logits", rows, vocab)
+    if dlogits.dtype != logits.dtype:
+        raise TypeError(f"dlogits must be {logits.dtype}, got {dlogits.dtype}")
+    op, ld_out = _logits_of(dlogits, "dlogits", rows, vocab)
+    _sized(_typed(targets, "targets", "int64"), "targets", rows)
+    _per_row(rows, row_max=row_max, log_sum=log_sum, entropy=entropy, dlogp=dlogp, dentropy=dentropy)
+    desc = hilore_token_logprobs_bwd_desc(lp, _p(targets), _p(row_max), _p(log_sum), _p(entropy), _p(dlogp),
+                                          _p(dentropy), op, rows, vocab, ld, ld_out, float(scale),
+                                          0 if logits.element_size() == 2 else 1)
+    return _on_device(desc, logits, targets, row_max, log_sum, entropy, dlogp, dentropy, dlogits)
+
+
+def hilore_token_logprobs_bwd(desc: hilore_token_logprobs_bwd_desc, stream=None):
+    """dlogits from the gradients of the targets' log-probabilities and of the entropies."""
+    _check("hilore_token_logprobs_bwd",
+           load().hilore_token_logprobs_bwd(_current(desc), _stream(stream)))
+
+
+def _per_token(n: int, dtype: str, **tensors):
+    for name, t in tensors.items():
+        if t is not None and _typed(t, name, *dtype.split("|")).numel() != n:
+            raise ValueError(f"{name} has {t.numel()} elements, logp {n}")
+
+
+def _sequences(logp, offsets, sequences) -> int:
+    """Number of sequences: as given, of the offsets, or the rows of a 2-D logp."""
+    if offsets is not None:
+        count = int(_typed(offsets, "offsets", "int64").numel()) - 1
+        if count < 0 or (sequences is not None and int(sequences) != count):
+            raise ValueError(f"offsets of {count} sequences, sequences = {sequences}")
+        return count
+    if sequences is None:
+        if logp.dim() != 2:
+            raise ValueError("without offsets give sequences, or logp as [sequences, length]")
+        return int(logp.shape[0])
+    return int(sequences)
+
+
+def policy_loss_desc(logp, logp_old, adv, logp_ref=None, entropy=None, mask=None, offsets=None,
+                     sequences=None, clip_low: float = _d.CLIP_EPS, clip_high: float = _d.CLIP_EPS,
+                     dual_clip: float = 0.0, beta: float = 0.0, entropy_weight: float = 0.0, kl: int = 0,
+                     ratio="token", mean="tokens", n_norm: float = 0.0, dlogp=None, dentropy=None,
+                     token_loss=None, flags=None, stats=None) -> hilore_policy_loss_desc:
+    """Descriptor of hilore_policy_loss: per-token tensors f32 of one size (any shape, dense), mask
+    and flags u8 or bool, adv f32 with one value a sequence or a token, offsets i64 [sequences + 1]
+    of packed sequences (None: `sequences` rows of equal length, or logp's rows), kl 0 (none) or 1, 2, 3 for
+    the estimators K1 to K3, stats f32 [8]."""
+    n = int(logp.numel())
+    count = _sequences(logp, offsets, sequences)
+    _per_token(n, "float32", logp=logp, logp_old=logp_old, logp_ref=logp_ref, entropy=entropy,
+               dlogp=dlogp, dentropy=dentropy, token_loss=token_loss)
+    _per_token(n, "uint8|bool", mask=mask, flags=flags)
+    if _typed(adv, "adv", "float32").numel() not in (count, n):
+        raise ValueError(f"adv needs {count} or {n} elements, got {adv.numel()}")
+    _sized(_typed(stats, "stats", "float32"), "stats", 8)
+    desc = hilore_policy_loss_desc(_p(logp), _p(logp_old), _p(logp_ref), _p(entropy), _p(adv), _p(mask),
+                                   _p(offsets), _p(dlogp), _p(dentropy), _p(token_loss), _p(flags), _p(stats),
+                                   n, count, float(n_norm), float(clip_low), float(clip_high),
+                                   float(dual_clip), float(beta), float(entropy_weight),
+                                   0 if adv.numel() == count else 1, _choice(ratio, RATIOS, "ratio"),
+                                   int(kl), _choice(mean, MEANS, "mean"))
+    return _on_device(desc, logp, logp_old, logp_ref, entropy, adv, mask, offsets, dlogp, dentropy,
+                      token_loss, flags, stats)
+
+
+def hilore_policy_loss_workspace_bytes(desc: hilore_policy_loss_desc) -> int:
+    return int(load().hilore_policy_loss_workspace_bytes(ctypes.byref(desc)))
+
+
+def hilore_policy_loss(desc: hilore_policy_loss_desc, workspace=None, stream=None):
+    """The clipped policy loss, its statistics and its gradients.  workspace: a device tensor of at
+    least hilore_policy_loss_workspace_bytes(desc) bytes, or None (taken from torch's allocator)."""
+    address = _current(desc)
+    need = hilore_policy_loss_workspace_bytes(desc) if workspace is None else 0
+    wp, wb, _keep = _workspace(workspace, need, stream)
+    _check("hilore_policy_loss", load().hilore_policy_loss(address, wp, wb, _stream(stream)))
+
+
+def preference_loss_desc(logp, logp_ref=None, mask=None, offsets=None, sequences=None, chosen=None,
+                         rejected=None, beta: float = 0.1, label_smoothing: float = 0.0,
+                         margin: float = 0.0, loss="logistic", length_mean: bool = False,
+                         n_norm: float = 0.0, dlogp=None, rewards=None, pair_loss=None,
+                         stats=None) -> hilore_preference_loss_desc:
+    """Descriptor of hilore_preference_loss: logp, logp_ref and dlogp f32 of one size, mask u8 or
+    bool, sequences as in policy_loss_desc, chosen and rejected i32 [pairs] (None: sequences 2p and 2p + 1), rewards f32
+    [sequences], pair_loss f32 [pairs], stats f32 [6]."""
+    n = int(logp.numel())
+    count = _sequences(logp, offsets, sequences)
+    _per_token(n, "float32", logp=logp, logp_ref=logp_ref, dlogp=dlogp)
+    _per_token(n, "uint8|bool", mask=mask)
+    if (chosen is None) != (rejected is None):
+        raise ValueError("chosen and rejected go together")
+    pairs = count // 2 if chosen is None else int(chosen.numel())
+    _sized(_typed(chosen, "chosen", "int32"), "chosen", pairs)
+    _sized(_typed(rejected, "rejected", "int32"), "rejected", pairs)
+    _sized(_typed(rewards, "rewards", "float32"), "rewards", count)
+    _sized(_typed(pair_loss, "pair_loss", "float32"), "pair_loss", pairs)
+    _sized(_typed(stats, "stats", "float32"), "stats", 6)
+    desc = hilore_preference_loss_desc(_p(logp), _p(logp_ref), _p(mask), _p(offsets), _p(chosen), _p(rejected),
+                                       _p(dlogp), _p(rewards), _p(pair_loss), _p(stats), n, count, pairs,
+                                       float(n_norm), float(beta), float(label_smoothing), float(margin),
+                                       _choice(loss, PREFERENCES, "loss"), 1 if length_mean else 0)
+    return _on_device(desc, logp, logp_ref, mask, offsets, chosen, rejected, dlogp, rewards, pair_loss, stats)
+
+
+def hilore_preference_loss_workspace_bytes(desc: hilore_preference_loss_desc) -> int:
+    return int(load().hilore_preference_loss_workspace_bytes(ctypes.byref(desc)))
+
+
+def hilore_preference_loss(desc: hilore_preference_loss_desc, workspace=None, stream=None):
+    """The preference loss over pairs of sequences, its statistics and its gradient.  workspace: a
+    device tensor of at least hilore_preference_loss_workspace_bytes(desc) bytes, or None (taken from
+    torch's allocator)."""
+    address = _current(desc)
+    need = hilore_preference_loss_workspace_bytes(desc) if workspace is None else 0
+    wp, wb, _keep = _workspace(workspace, need, stream)
+    _check("hilore_preference_loss", load().hilore_preference_loss(address, wp, wb, _stream(stream)))
