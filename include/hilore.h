@@ -902,8 +902,8 @@ typedef enum hilore_mean {
  *            the n_i tokens of the sequence share it)
  * Sequences: rows of equal length n_tokens / sequences one after another, or with
  * offsets i64 [sequences + 1] (nondecreasing, within [0, n_tokens]) sequence i is the
- * tokens [offsets[i], offsets[i + 1]), possibly none.  Tokens of no sequence are neither
- * read nor written.
+ * tokens [offsets[i], offsets[i + 1]), possibly none.  Tokens of no sequence count for
+ * nothing and their outputs are left as they were.
  *   logp, logp_old, logp_ref, entropy  f32 [n_tokens]; logp_ref only (and always) with a kl,
  *            entropy NULL: no bonus (entropy_weight 0, dentropy NULL)
  *   adv      f32 [sequences], or (adv_per_token != 0) [n_tokens], then with HILORE_RATIO_TOKEN
@@ -916,7 +916,8 @@ typedef enum hilore_mean {
  * [n_tokens], 0 where masked; flags u8 [n_tokens]: bit 0 valid and chi, bit 1 valid, A != 0
  * and not chi; stats f32 [8]: loss, weighted sums of policy, kl and entropy, share of the
  * valid tokens with flag bit 1, their mean ratio, their number, the sequences that have any.
- * Per-token arithmetic in fp32, sums over tokens in fp64 in a fixed order.
+ * Per-token arithmetic in fp32; statistics are summed in fp32 over at most 256 tokens and in fp64
+ * beyond, a sequence's mean in fp64, all in a fixed order.
  * workspace: device memory of at least hilore_policy_loss_workspace_bytes(d) bytes, 16-byte
  * aligned, contents on entry irrelevant; calls sharing it must not overlap.
  * Limits: n_tokens < 2^31, sequences < 2^31.

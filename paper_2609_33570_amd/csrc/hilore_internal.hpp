@@ -449,7 +449,7 @@ struct PolicyArgs {
   float bound_high, bound_low, log_high, log_low, dual, log_dual;
   float beta, bonus;
   int adv_per_token, sequence_ratio, kl, sequence_mean;
-  uint32_t *count;           // workspace: valid tokens of each sequence
+  double *share;             // workspace, by sequence: 1 / its valid tokens
   float *mean_delta;         // and their mean log ratio
   double *part;              // partial sums
 };
