@@ -717,7 +717,7 @@ typedef enum hilore_rotation {
  *              projection's rows); heads_k may be 0 (k fields unused)
  *   w_q, w_k   bf16 [dim]; NULL: no norm of the queries' / keys' heads
  *   positions  i64 [tokens]; NULL: t.  A negative position is padding: the token's inputs
- *              are not read and its outputs are 0
+ *              are not used (they may be NaN) and its outputs are 0
  *   inv_freq   f32 [rotated / 2]; not read where rotated is 0
  * Outputs: q_out, k_out bf16, column c of head j of token t at t * token_stride +
  * j * head_stride + c: [tokens, heads, dim] or [heads, tokens, dim], dense or padded.
@@ -767,7 +767,7 @@ hilore_status hilore_qk_norm_rope(const hilore_qk_norm_rope_desc *d, void *strea
  * Outputs: dq_in, dk_in bf16 [tokens, heads * dim], row strides ld_dq and ld_dk (a slice of
  * the projection's gradient); dq_in may be dq where the strides agree; NULL: not wanted.
  * dw_q, dw_k f32 [dim] or NULL; accumulate != 0 adds to what is there.
- * Tokens with a negative position get 0 and give dw nothing (their rows are not read).
+ * Tokens with a negative position get 0 and give dw nothing, whatever their rows hold.
  * workspace: device memory of at least hilore_qk_norm_rope_bwd_workspace_bytes(d) bytes (0, and
  * then NULL is allowed, without dw), 16-byte aligned, contents on entry irrelevant; calls
  * sharing it must not overlap.  Sums over tokens and heads in a fixed order.

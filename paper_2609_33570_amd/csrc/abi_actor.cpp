@@ -357,7 +357,7 @@ hilore_status hilore_qk_norm_rope(const hilore_qk_norm_rope_desc *d, void *strea
 
 size_t hilore_qk_norm_rope_bwd_workspace_bytes(const hilore_qk_norm_rope_bwd_desc *d) {
   if (!d || check_head_sizes(*d) != HILORE_OK || (!d->dw_q && !d->dw_k)) return 0;
-  return (size_t)2 * (size_t)hilore::heads_bwd_groups(d->tokens, d->heads_q + d->heads_k, d->dim) * (size_t)d->dim *
+  return (size_t)2 * (size_t)hilore::heads_bwd_groups(d->tokens, d->heads_q + d->heads_k, d->dim, 1) * (size_t)d->dim *
          sizeof(float);
 }
 
@@ -377,7 +377,7 @@ hilore_status hilore_qk_norm_rope_bwd(const hilore_qk_norm_rope_bwd_desc *d, int
   a.accumulate = accumulate ? 1 : 0;
   a.code = code;
   a.block_log2 = log2_of(block);
-  a.groups = hilore::heads_bwd_groups(d->tokens, d->heads_q + d->heads_k, d->dim);
+  a.groups = hilore::heads_bwd_groups(d->tokens, d->heads_q + d->heads_k, d->dim, d->dw_q || d->dw_k);
   a.part = static_cast<float *>(workspace);
   return hip_status(hilore::launch_heads_bwd(a, static_cast<hipStream_t>(stream)));
 }

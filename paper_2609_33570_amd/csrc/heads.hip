@@ -108,7 +108,9 @@ __device__ __forceinline__ void rotate(float x[16], const Angles &g, bool pairs)
 }
 
 __device__ __forceinline__ u32x4 load16(const uint16_t *p) { return *reinterpret_cast<const u32x4 *>(p); }
-__device__ __forceinline__ void store16(uint16_t *p, u32x4 v) { *reinterpret_cast<u32x4 *>(p) = v; }
+__device__ __forceinline__ void store16(uint16_t *p, u32x4 v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p));
+}
 
 __device__ __forceinline__ void unpack16(u32x4 a, u32x4 b, float x[16]) {
   unpack_bf16x8(a, x);
@@ -151,20 +153,23 @@ __global__ __launch_bounds__(kWaves *kWave) void heads_kernel(const HeadsArgs h,
     const int part = (int)(unit - token * parts);
     const int first = part * per, last = min(first + per, steps);
     const int64_t position = h.positions ? h.positions[token] : token;
-    if (position >= 0) angles(h, position, cs[wave], sn[wave]);
-    const Angles ang = lane_angles(cs[wave], sn[wave], at);
+    Angles ang;
     for (int step = first; step < last; step += kForwardSteps) {
       u32x4 xa[kForwardSteps], xb[kForwardSteps];
 #pragma unroll
       for (int i = 0; i < kForwardSteps; ++i) {
         const int head = (step + i) * kSide + lane / G;
         xa[i] = xb[i] = u32x4{};
-        if (step + i >= last || head >= heads || !at.live || position < 0) continue;
+        if (step + i >= last || head >= heads || !at.live) continue;
         const bool key = head >= h.heads_q;
         const uint16_t *x = key ? h.k.in.x + token * h.k.in.ld + (int64_t)(head - h.heads_q) * h.dim
                                 : h.q.in.x + token * h.q.in.ld + (int64_t)head * h.dim;
         xa[i] = load16(x + at.a);
         xb[i] = load16(x + at.b);
+      }
+      if (step == first) {  // while the first heads are on their way
+        if (position >= 0) angles(h, position, cs[wave], sn[wave]);
+        ang = lane_angles(cs[wave], sn[wave], at);
       }
 #pragma unroll
       for (int i = 0; i < kForwardSteps; ++i) {
@@ -233,10 +238,54 @@ struct SavedHead {
   Saved8<K> ka, kb;
 };
 
-constexpr int kBackwardSteps = 2;
+constexpr int kBackwardSteps = 1;  // heads a group has in flight while it works on as many
+
+// What the backward reads of some of a token's heads.
+template <int Q, int K>
+struct BackwardHeads {
+  u32x4 ga[kBackwardSteps], gb[kBackwardSteps];
+  SavedHead<Q, K> saved[kBackwardSteps];
+};
+
+template <int G, int Q, int K>
+__device__ __forceinline__ void load_heads(BackwardHeads<Q, K> &x, const HeadsArgs &h, const Place &at, int64_t token, int step, int last) {
+  constexpr int kSide = kWave / G;
+  const int lane = threadIdx.x & 63, heads = h.heads_q + h.heads_k;
+#pragma unroll
+  for (int i = 0; i < kBackwardSteps; ++i) {
+    const int head = (step + i) * kSide + lane / G;
+    x.ga[i] = x.gb[i] = u32x4{};
+    x.saved[i] = SavedHead<Q, K>{};
+    if (step + i >= last || head >= heads || !at.live) continue;
+    const bool key = head >= h.heads_q;
+    const int j = key ? head - h.heads_q : head;
+    const uint16_t *g = key ? h.k.g + token * h.k.token_stride + j * h.k.head_stride
+                            : h.q.g + token * h.q.token_stride + j * h.q.head_stride;
+    x.ga[i] = load16(g + at.a);
+    x.gb[i] = load16(g + at.b);
+    const int64_t col = (int64_t)j * h.dim;
+    if constexpr (Q == K) {  // the sides differ in their addresses alone
+      if (!(key ? h.k.w : h.q.w)) continue;
+      const int64_t cols = (int64_t)(key ? h.heads_k : h.heads_q) * h.dim;
+      const SavedRows in = {key ? h.k.in.x : h.q.in.x, key ? h.k.in.codes : h.q.in.codes, key ? h.k.in.scales : h.q.in.scales,
+                            key ? h.k.in.ld : h.q.in.ld};
+      load_saved<Q>(x.saved[i].qa, in, token, cols, col + at.a, h.block_log2);
+      load_saved<Q>(x.saved[i].qb, in, token, cols, col + at.b, h.block_log2);
+    } else if (key) {
+      if (!h.k.w) continue;
+      const int64_t cols = (int64_t)h.heads_k * h.dim;
+      load_saved<K>(x.saved[i].ka, h.k.in, token, cols, col + at.a, h.block_log2);
+      load_saved<K>(x.saved[i].kb, h.k.in, token, cols, col + at.b, h.block_log2);
+    } else if (h.q.w) {
+      const int64_t cols = (int64_t)h.heads_q * h.dim;
+      load_saved<Q>(x.saved[i].qa, h.q.in, token, cols, col + at.a, h.block_log2);
+      load_saved<Q>(x.saved[i].qb, h.q.in, token, cols, col + at.b, h.block_log2);
+    }
+  }
+}
 
 template <int G, int Q, int K, bool SUMS>
-__global__ __launch_bounds__(kWaves *kWave) void heads_bwd_kernel(const HeadsArgs h, int parts) {
+__global__ __launch_bounds__(kWaves *kWave, SUMS ? (Q == K ? 3 : 2) : 4) void heads_bwd_kernel(const HeadsArgs h, int parts) {
   __shared__ float cs[kWaves][kHeadMaxDim / 2], sn[kWaves][kHeadMaxDim / 2];
   constexpr int kSide = kWave / G;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -249,88 +298,79 @@ __global__ __launch_bounds__(kWaves *kWave) void heads_bwd_kernel(const HeadsArg
   if constexpr (SUMS)
 #pragma unroll
     for (int c = 0; c < 16; ++c) sq[c] = sk[c] = 0.0f;
-  const int64_t units = h.tokens * parts;
-  for (int64_t unit = (int64_t)blockIdx.x * kWaves + wave; unit < units; unit += (int64_t)gridDim.x * kWaves) {
+  const int64_t units = h.tokens * parts, stride = (int64_t)gridDim.x * kWaves;
+  int64_t unit = (int64_t)blockIdx.x * kWaves + wave;
+  BackwardHeads<Q, K> next;
+  int64_t position = 0;
+  if (unit < units) {
     const int64_t token = unit / parts;
-    const int part = (int)(unit - token * parts);
-    const int first = part * per, last = min(first + per, steps);
-    const int64_t position = h.positions ? h.positions[token] : token;
-    if (position >= 0) angles(h, position, cs[wave], sn[wave]);
+    const int first = (int)(unit - token * parts) * per;
+    position = h.positions ? h.positions[token] : token;
+    load_heads<G, Q, K>(next, h, at, token, first, min(first + per, steps));
+  }
+  for (; unit < units; unit += stride) {
+    const int64_t token = unit / parts;
+    const int first = (int)(unit - token * parts) * per, last = min(first + per, steps);
+    const bool pad = position < 0;
+    if (!pad) angles(h, position, cs[wave], sn[wave]);
     const Angles ang = lane_angles(cs[wave], sn[wave], at);
+    // the next unit's first heads are loaded behind this one's last ones
+    const int64_t unit2 = unit + stride < units ? unit + stride : unit, token2 = unit2 / parts;
+    const int first2 = (int)(unit2 - token2 * parts) * per;
+    position = h.positions ? h.positions[token2] : token2;
     for (int step = first; step < last; step += kBackwardSteps) {
-      u32x4 ga[kBackwardSteps], gb[kBackwardSteps];
-      SavedHead<Q, K> saved[kBackwardSteps];
-#pragma unroll
-      for (int i = 0; i < kBackwardSteps; ++i) {
-        const int head = (step + i) * kSide + lane / G;
-        ga[i] = gb[i] = u32x4{};
-        saved[i] = SavedHead<Q, K>{};
-        if (step + i >= last || head >= heads || !at.live || position < 0) continue;
-        const bool key = head >= h.heads_q;
-        const int j = key ? head - h.heads_q : head;
-        const uint16_t *g = key ? h.k.g + token * h.k.token_stride + j * h.k.head_stride
-                                : h.q.g + token * h.q.token_stride + j * h.q.head_stride;
-        ga[i] = load16(g + at.a);
-        gb[i] = load16(g + at.b);
-        const int64_t col = (int64_t)j * h.dim;
-        if (key) {
-          if (h.k.w) {
-            const int64_t cols = (int64_t)h.heads_k * h.dim;
-            load_saved<K>(saved[i].ka, h.k.in, token, cols, col + at.a, h.block_log2);
-            load_saved<K>(saved[i].kb, h.k.in, token, cols, col + at.b, h.block_log2);
-          }
-        } else if (h.q.w) {
-          const int64_t cols = (int64_t)h.heads_q * h.dim;
-          load_saved<Q>(saved[i].qa, h.q.in, token, cols, col + at.a, h.block_log2);
-          load_saved<Q>(saved[i].qb, h.q.in, token, cols, col + at.b, h.block_log2);
-        }
-      }
+      const BackwardHeads<Q, K> now = next;
+      const bool more = step + kBackwardSteps < last;
+      load_heads<G, Q, K>(next, h, at, more ? token : token2, more ? step + kBackwardSteps : first2, more ? last : min(first2 + per, steps));
 #pragma unroll
       for (int i = 0; i < kBackwardSteps; ++i) {
         if (step + i >= last) break;
-        const int head = (step + i) * kSide + lane / G;
+        const int head0 = (step + i) * kSide, head = head0 + lane / G;
         const bool key = head >= h.heads_q;
         float g[16];
-        unpack16(ga[i], gb[i], g);
+        unpack16(now.ga[i], now.gb[i], g);
         if (at.turned) rotate<true>(g, ang, h.pairs);
-        float x[16], wv[16];
-        if (key) {
-          saved_values<K>(saved[i].ka, x);
-          saved_values<K>(saved[i].kb, x + 8);
-        } else {
-          saved_values<Q>(saved[i].qa, x);
-          saved_values<Q>(saved[i].qb, x + 8);
-        }
-        float ss = 0.0f, sx = 0.0f;
-        unpack16(key ? w.k[0] : w.q[0], key ? w.k[1] : w.q[1], wv);
-#pragma unroll
-        for (int c = 0; c < 16; ++c) {
-          ss = fmaf(x[c], x[c], ss);
-          sx = fmaf(g[c] * wv[c], x[c], sx);
-        }
-        ss = group_sum<G>(ss);
-        sx = group_sum<G>(sx);
-        const bool inside = head < heads && at.live && position >= 0;
+        const bool inside = head < heads && at.live && !pad;
         if (key ? h.k.w != nullptr : h.q.w != nullptr) {
+          float x[16], t[16];
+          if (Q == K || !key) {
+            saved_values<Q>(now.saved[i].qa, x);
+            saved_values<Q>(now.saved[i].qb, x + 8);
+          } else {
+            saved_values<K>(now.saved[i].ka, x);
+            saved_values<K>(now.saved[i].kb, x + 8);
+          }
+          unpack16(key ? w.k[0] : w.q[0], key ? w.k[1] : w.q[1], t);
+          float ss = 0.0f, sx = 0.0f;
+#pragma unroll
+          for (int c = 0; c < 16; ++c) {
+            t[c] = g[c] * t[c];
+            ss = fmaf(x[c], x[c], ss);
+            sx = fmaf(t[c], x[c], sx);
+          }
+          // a head's lanes are all of one side, so all of them are here
+          ss = group_sum<G>(ss);
+          sx = group_sum<G>(sx);
           const float r = __builtin_amdgcn_rsqf(ss * h.inv_dim + h.eps);
-          const float along = r * r * (sx * h.inv_dim);
+          const float along = r * (sx * h.inv_dim);
+#pragma unroll
+          for (int c = 0; c < 16; ++c) x[c] *= r;
           if constexpr (SUMS)
             if (inside) {
+              if (key)
 #pragma unroll
-              for (int c = 0; c < 16; ++c) {
-                const float d = g[c] * (x[c] * r);
-                sq[c] += key ? 0.0f : d;
-                sk[c] += key ? d : 0.0f;
-              }
+                for (int c = 0; c < 16; ++c) sk[c] = fmaf(g[c], x[c], sk[c]);
+              else
+#pragma unroll
+                for (int c = 0; c < 16; ++c) sq[c] = fmaf(g[c], x[c], sq[c]);
             }
 #pragma unroll
-          for (int c = 0; c < 16; ++c) g[c] = r * fmaf(-along, x[c], g[c] * wv[c]);
+          for (int c = 0; c < 16; ++c) g[c] = r * fmaf(-along, x[c], t[c]);
         }
         if (head >= heads || !at.live) continue;
         uint16_t *out = key ? h.k.out : h.q.out;
         if (!out) continue;
         out += token * (key ? h.k.ld_out : h.q.ld_out) + (int64_t)(key ? head - h.heads_q : head) * h.dim;
-        const bool pad = position < 0;
         store16(out + at.a, pad ? u32x4{} : pack_bf16x8(g));
         store16(out + at.b, pad ? u32x4{} : pack_bf16x8(g + 8));
       }
@@ -372,7 +412,7 @@ __global__ __launch_bounds__(kFoldWaves *kWave) void heads_fold_kernel(const Hea
   float sum = 0.0f;
   if (col < h.dim) {
     const float *p = h.part + ((int64_t)blockIdx.y * h.groups) * h.dim + col;
-#pragma unroll 8
+#pragma unroll 16
     for (int g = wave; g < h.groups; g += kFoldWaves) sum += p[(int64_t)g * h.dim];
   }
   lds[wave][lane] = sum;
@@ -448,10 +488,11 @@ hipError_t launch_heads(const HeadsArgs &h, hipStream_t s) {
   return hipGetLastError();
 }
 
-int heads_bwd_groups(int64_t tokens, int heads, int dim) {
+int heads_bwd_groups(int64_t tokens, int heads, int dim, int sums) {
   if (tokens == 0 || heads == 0) return 0;
   const int64_t need = (tokens * parts_of(tokens, heads, dim) + kWaves - 1) / kWaves;
-  return (int)(need < 1024 ? need : 1024);
+  const int most = sums ? 768 : 1024;
+  return (int)(need < most ? need : most);
 }
 
 hipError_t launch_heads_bwd(const HeadsArgs &h, hipStream_t s) {

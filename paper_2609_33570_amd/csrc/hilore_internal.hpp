@@ -406,7 +406,7 @@ struct HeadsArgs {
   int groups;                // backward with dw: workgroups, each with a row of partial sums
   float *part;               // [q, k][group][dim]
 };
-int heads_bwd_groups(int64_t tokens, int heads, int dim);
+int heads_bwd_groups(int64_t tokens, int heads, int dim, int sums);
 hipError_t launch_heads(const HeadsArgs &a, hipStream_t s);
 hipError_t launch_heads_bwd(const HeadsArgs &a, hipStream_t s);
 

@@ -35,8 +35,8 @@ typedef u32x4 __attribute__((aligned(4))) u32x4_f32;
 
 template <bool F32>
 __device__ __forceinline__ u32x4 load_piece(const void *row, int64_t piece) {
-  if constexpr (F32) return *reinterpret_cast<const u32x4_f32 *>(static_cast<const float *>(row) + piece * 4);
-  else return *reinterpret_cast<const u32x4_bf16 *>(static_cast<const uint16_t *>(row) + piece * 8);
+  if constexpr (F32) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_f32 *>(static_cast<const float *>(row) + piece * 4));
+  else return __builtin_nontemporal_load(reinterpret_cast<const u32x4_bf16 *>(static_cast<const uint16_t *>(row) + piece * 8));
 }
 
 template <bool F32>
@@ -270,8 +270,8 @@ constexpr int kBwdChunk = kThreads * kBwdPieces;
 
 template <bool F32>
 __device__ __forceinline__ void store_piece(void *row, int64_t piece, u32x4 w) {
-  if constexpr (F32) *reinterpret_cast<u32x4_f32 *>(static_cast<float *>(row) + piece * 4) = w;
-  else *reinterpret_cast<u32x4_bf16 *>(static_cast<uint16_t *>(row) + piece * 8) = w;
+  if constexpr (F32) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_f32 *>(static_cast<float *>(row) + piece * 4));
+  else __builtin_nontemporal_store(w, reinterpret_cast<u32x4_bf16 *>(static_cast<uint16_t *>(row) + piece * 8));
 }
 
 // What a row's gradient is made of.
