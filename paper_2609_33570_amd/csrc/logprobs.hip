@@ -33,10 +33,12 @@ constexpr float kLn2 = 0.6931471805599453f;
 typedef u32x4 __attribute__((aligned(2))) u32x4_bf16;
 typedef u32x4 __attribute__((aligned(4))) u32x4_f32;
 
+// The row's address is the same in all lanes and a piece's place in it fits 32 bits (vocab < 2^28).
 template <bool F32>
-__device__ __forceinline__ u32x4 load_piece(const void *row, int64_t piece) {
-  if constexpr (F32) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_f32 *>(static_cast<const float *>(row) + piece * 4));
-  else return __builtin_nontemporal_load(reinterpret_cast<const u32x4_bf16 *>(static_cast<const uint16_t *>(row) + piece * 8));
+__device__ __forceinline__ u32x4 load_piece(const void *row, int piece) {
+  const char *p = static_cast<const char *>(row) + (uint32_t)piece * 16u;
+  if constexpr (F32) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_f32 *>(p));
+  else return __builtin_nontemporal_load(reinterpret_cast<const u32x4_bf16 *>(p));
 }
 
 template <bool F32>
@@ -110,7 +112,9 @@ __device__ __forceinline__ float lanes_max(float v) {
   return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
-// NaN stays in the sums: only the maximum and the entropy's factor pass it by.
+// One batch of a lane.  NaN stays in the sums: only the maximum and the entropy's factor pass it by.  The way to
+// the maximum is a difference before it is scaled: exact for near logits and finite for those of the type's
+// lowest value (c z - c m in one step was 3 % faster, 8192 x 131072 in 320 us, but off by a step of c m).
 template <bool F32, bool ENTROPY>
 __device__ __forceinline__ void take(State &x, const u32x4 (&w)[kBatch], float c) {
   constexpr int E = kPiece<F32>;
@@ -137,20 +141,20 @@ __device__ __forceinline__ void take(State &x, const u32x4 (&w)[kBatch], float c
 
 // This wave's part of one segment of a row, the chosen token left out.
 template <bool F32, bool ENTROPY>
-__device__ __forceinline__ State segment_state(const void *row, int64_t vocab, int64_t segment, int64_t target, float c) {
+__device__ __forceinline__ State segment_state(const void *row, int vocab, int segment, int target, float c) {
   constexpr int E = kPiece<F32>;
-  const int64_t pieces = vocab / E, chosen = target / E;
-  const int64_t begin = segment * kSegment;
+  const int pieces = vocab / E, chosen = target / E;
+  const int begin = segment * kSegment, mine = begin + (int)threadIdx.x;
   State x = nothing();
   if (begin + kSegment <= pieces) {
 #pragma unroll
     for (int b = 0; b < kBatches; ++b) {
       u32x4 w[kBatch];
 #pragma unroll
-      for (int p = 0; p < kBatch; ++p) w[p] = load_piece<F32>(row, begin + (b * kBatch + p) * kThreads + threadIdx.x);
+      for (int p = 0; p < kBatch; ++p) w[p] = load_piece<F32>(row, mine + (b * kBatch + p) * kThreads);
 #pragma unroll
       for (int p = 0; p < kBatch; ++p)
-        if (begin + (b * kBatch + p) * kThreads + threadIdx.x == chosen) w[p] = without<F32>(w[p], (int)(target - chosen * E));
+        if (mine + (b * kBatch + p) * kThreads == chosen) w[p] = without<F32>(w[p], target - chosen * E);
       take<F32, ENTROPY>(x, w, c);
     }
   } else {
@@ -159,16 +163,16 @@ __device__ __forceinline__ State segment_state(const void *row, int64_t vocab, i
       u32x4 w[kBatch];
 #pragma unroll
       for (int p = 0; p < kBatch; ++p) {
-        const int64_t piece = begin + (b * kBatch + p) * kThreads + threadIdx.x;
+        const int piece = mine + (b * kBatch + p) * kThreads;
         w[p] = piece_of<F32>(-__builtin_inff());
         if (piece < pieces) w[p] = load_piece<F32>(row, piece);
-        if (piece == chosen) w[p] = without<F32>(w[p], (int)(target - chosen * E));
+        if (piece == chosen) w[p] = without<F32>(w[p], target - chosen * E);
       }
       take<F32, ENTROPY>(x, w, c);
     }
   }
   if (begin + kSegment >= pieces) {  // the last segment: what is left behind the last whole piece
-    const int64_t i = pieces * E + threadIdx.x;
+    const int i = pieces * E + (int)threadIdx.x;
     if (i < vocab && i != target) {
       const float z = load_one<F32>(row, i), m = fmaxf(x.m, z);
       x = seen(x, m, c);
@@ -181,21 +185,23 @@ __device__ __forceinline__ State segment_state(const void *row, int64_t vocab, i
   return State{y.m, lanes_sum(y.s), ENTROPY ? lanes_sum(y.t) : 0.0f};
 }
 
-// The row's outputs from the state of all its tokens but the chosen one.
+// A row's chosen token and its logit (-inf where there is none).
 template <bool F32>
-__device__ __forceinline__ void finish(const LogprobsArgs &a, int64_t row, const State &others, float c) {
-  const int64_t target = a.targets[row];
+__device__ __forceinline__ float chosen_logit(const LogprobsArgs &a, int64_t row, int64_t target) {
+  const void *z = static_cast<const char *>(a.logits) + row * a.ld * (F32 ? 4 : 2);
+  return target >= 0 && target < a.vocab ? load_one<F32>(z, target) : -__builtin_inff();
+}
+
+// The row's outputs from the chosen token's logit and the state of all others.
+__device__ __forceinline__ void finish(const LogprobsArgs &a, int64_t row, int64_t target, float zt, const State &others, float c) {
   float logp = 0.0f, entropy = 0.0f, m = 0.0f, log_sum = 0.0f;
   if (target >= 0) {
-    const void *z = static_cast<const char *>(a.logits) + row * a.ld * (F32 ? 4 : 2);
-    const bool inside = target < a.vocab;
-    const float zt = inside ? load_one<F32>(z, target) : -__builtin_inff();
     m = fmaxf(others.m, zt);
     const State x = seen(others, m, c);
     const float way = zt - m, d = c * way, e = __builtin_amdgcn_exp2f(d), sum = x.s + e;
     // the others alone where the chosen token is the largest: exact however small they are
     log_sum = way == 0.0f ? log1pf(x.s) : logf(sum);
-    logp = inside ? a.scale * way - log_sum : __builtin_nanf("");
+    logp = target < a.vocab ? a.scale * way - log_sum : __builtin_nanf("");
     entropy = log_sum - kLn2 * (fmaf(e, fmaxf(d, kNoWay), x.t) / sum);
     if (sum == 0.0f) m = -__builtin_inff();
   }
@@ -216,9 +222,10 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobsArgs a
     const int64_t row = a.split ? unit / segments : unit;
     const int64_t target = a.targets[row];
     const void *z = static_cast<const char *>(a.logits) + row * a.ld * (F32 ? 4 : 2);
+    const int place = target < a.vocab ? (int)target : (int)a.vocab;  // none is taken out past the end
     if (a.split) {
       if (target < 0) continue;
-      const State x = segment_state<F32, ENTROPY>(z, a.vocab, unit - row * segments, target, c);
+      const State x = segment_state<F32, ENTROPY>(z, (int)a.vocab, (int)(unit - row * segments), place, c);
       if ((threadIdx.x & 63) == 0) {
         float *o = a.part + (unit * kWaves + wave) * 4;
         o[0] = x.m;
@@ -227,15 +234,16 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobsArgs a
       }
       continue;
     }
+    const float zt = chosen_logit<F32>(a, row, target);
     State x = nothing();
     if (target >= 0)
-      for (int g = 0; g < segments; ++g) x = join(x, segment_state<F32, ENTROPY>(z, a.vocab, g, target, c), c);
+      for (int g = 0; g < segments; ++g) x = join(x, segment_state<F32, ENTROPY>(z, (int)a.vocab, g, place, c), c);
     if ((threadIdx.x & 63) == 0) lds[turn][wave] = x;
     __syncthreads();
     if (threadIdx.x == 0) {
       x = lds[turn][0];
       for (int w = 1; w < kWaves; ++w) x = join(x, lds[turn][w], c);
-      finish<F32>(a, row, x, c);
+      finish(a, row, target, zt, x, c);
     }
   }
 }
@@ -247,8 +255,13 @@ __global__ __launch_bounds__(kWave) void logprobs_join_kernel(const LogprobsArgs
   const int64_t row = (int64_t)blockIdx.x * (kWave / kWaves) + threadIdx.x / kWaves;
   const int wave = threadIdx.x % kWaves;
   State x = nothing();
-  if (row < a.rows && a.targets[row] >= 0) {
+  int64_t target = -1;
+  float zt = 0.0f;
+  if (row < a.rows) {
+    // the segments of a row without a token hold anything, and are not used
     const float *p = a.part + (row * segments * kWaves + wave) * 4;
+    target = a.targets[row];
+    zt = chosen_logit<F32>(a, row, target);
 #pragma unroll 4
     for (int g = 0; g < segments; ++g) {
       const float *q = p + (int64_t)g * kWaves * 4;
@@ -261,7 +274,7 @@ __global__ __launch_bounds__(kWave) void logprobs_join_kernel(const LogprobsArgs
     const State y = {__shfl(x.m, from), __shfl(x.s, from), __shfl(x.t, from)};
     all = join(all, y, c);
   }
-  if (wave == 0 && row < a.rows) finish<F32>(a, row, all, c);
+  if (wave == 0 && row < a.rows) finish(a, row, target, zt, all, c);
 }
 
 // --------------------------------------------------------------- backward --
@@ -269,9 +282,10 @@ constexpr int kBwdPieces = 8;  // of a lane
 constexpr int kBwdChunk = kThreads * kBwdPieces;
 
 template <bool F32>
-__device__ __forceinline__ void store_piece(void *row, int64_t piece, u32x4 w) {
-  if constexpr (F32) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_f32 *>(static_cast<float *>(row) + piece * 4));
-  else __builtin_nontemporal_store(w, reinterpret_cast<u32x4_bf16 *>(static_cast<uint16_t *>(row) + piece * 8));
+__device__ __forceinline__ void store_piece(void *row, int piece, u32x4 w) {
+  char *p = static_cast<char *>(row) + (uint32_t)piece * 16u;
+  if constexpr (F32) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_f32 *>(p));
+  else __builtin_nontemporal_store(w, reinterpret_cast<u32x4_bf16 *>(p));
 }
 
 // What a row's gradient is made of.
@@ -304,10 +318,11 @@ __device__ __forceinline__ float chosen_gradient(const RowGradient &r, float z) 
 template <bool F32, bool ENTROPY>
 __global__ __launch_bounds__(kThreads) void logprobs_bwd_kernel(const LogprobsBwdArgs a, int chunks) {
   constexpr int E = kPiece<F32>;
-  const int64_t units = a.rows * chunks, pieces = a.vocab / E;
+  const int64_t units = a.rows * chunks;
+  const int vocab = (int)a.vocab, pieces = vocab / E;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const int64_t row = unit / chunks;
-    const int64_t begin = (unit - row * chunks) * kBwdChunk;
+    const int begin = (int)(unit - row * chunks) * kBwdChunk, mine = begin + (int)threadIdx.x;
     const void *z = static_cast<const char *>(a.logits) + row * a.ld * (F32 ? 4 : 2);
     void *out = static_cast<char *>(a.dlogits) + row * a.ld_out * (F32 ? 4 : 2);
     const int64_t target = a.targets[row];
@@ -315,14 +330,14 @@ __global__ __launch_bounds__(kThreads) void logprobs_bwd_kernel(const LogprobsBw
     r.g = a.dlogp[row];
     if constexpr (ENTROPY) r.e = a.dentropy[row];
     const bool last = begin + kBwdChunk >= pieces;
-    const int64_t rest = pieces * E + threadIdx.x;  // behind the last whole piece
+    const int rest = pieces * E + (int)threadIdx.x;  // behind the last whole piece
     if (target < 0 || (r.g == 0.0f && r.e == 0.0f && target < a.vocab)) {
 #pragma unroll
       for (int p = 0; p < kBwdPieces; ++p) {
-        const int64_t piece = begin + p * kThreads + threadIdx.x;
+        const int piece = mine + p * kThreads;
         if (piece < pieces) store_piece<F32>(out, piece, u32x4{});
       }
-      if (last && rest < a.vocab) {
+      if (last && rest < vocab) {
         if constexpr (F32) static_cast<float *>(out)[rest] = 0.0f;
         else static_cast<uint16_t *>(out)[rest] = 0;
       }
@@ -331,7 +346,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_bwd_kernel(const LogprobsBw
     u32x4 w[kBwdPieces];
 #pragma unroll
     for (int p = 0; p < kBwdPieces; ++p) {
-      const int64_t piece = begin + p * kThreads + threadIdx.x;
+      const int piece = mine + p * kThreads;
       w[p] = u32x4{};
       if (piece < pieces) w[p] = load_piece<F32>(z, piece);
     }
@@ -342,11 +357,10 @@ __global__ __launch_bounds__(kThreads) void logprobs_bwd_kernel(const LogprobsBw
     r.c = a.scale * 1.4426950408889634f;
     r.log2_sum = r.log_sum * 1.4426950408889634f;
     if (target >= a.vocab) r.g = __builtin_nanf("");
-    const int64_t chosen = target / E;
-    const int place = (int)(target - chosen * E);
+    const int at = target < vocab ? (int)target : vocab, chosen = at / E, place = at - chosen * E;
 #pragma unroll
     for (int p = 0; p < kBwdPieces; ++p) {
-      const int64_t piece = begin + p * kThreads + threadIdx.x;
+      const int piece = mine + p * kThreads;
       if (piece >= pieces) continue;
       float v[E], d[E];
       values<F32>(w[p], v);
@@ -362,7 +376,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_bwd_kernel(const LogprobsBw
       else o = pack_bf16x8(d);
       store_piece<F32>(out, piece, o);
     }
-    if (last && rest < a.vocab) {
+    if (last && rest < vocab) {
       const float v = load_one<F32>(z, rest);
       const float d = a.scale * (rest == target ? chosen_gradient<ENTROPY>(r, v) : gradient<ENTROPY>(r, v));
       if constexpr (F32) static_cast<float *>(out)[rest] = d;
