@@ -52,14 +52,20 @@ __device__ __forceinline__ Place place(const HeadsArgs &h, int p) {
   return at;
 }
 
-// The token's cosines and sines times rope_scale, to the wave's part of LDS.  The angle in turns is a
+// The token's cosines and sines times rope_scale, to the wave's part of LDS (freq: first_freq).  The angle in turns is a
 // product of two fp64 pairs (position * inv_freq and 1 / 2 pi with what their rounding leaves), so that
 // positions up to 2^53 turn as exactly as near ones: the fraction is rounded once, to 2^-25 of a turn.
-__device__ __forceinline__ void angles(const HeadsArgs &h, int64_t position, float *cs, float *sn) {
+// first_freq: inv_freq[lane], read once by every wave (0 past its end).
+__device__ __forceinline__ float first_freq(const HeadsArgs &h) {
+  const int lane = threadIdx.x & 63;
+  return lane < h.rotated / 2 ? h.inv_freq[lane] : 0.0f;
+}
+
+__device__ __forceinline__ void angles(const HeadsArgs &h, int64_t position, float freq, float *cs, float *sn) {
   constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57;  // 1 / 2 pi
   const int half = h.rotated / 2, lane = threadIdx.x & 63;
   for (int i = lane; i < half; i += kWave) {
-    const double p = (double)position, f = (double)h.inv_freq[i];
+    const double p = (double)position, f = (double)(i < kWave ? freq : h.inv_freq[i]);
     const double a = p * f, a_rest = fma(p, f, -a);
     const double turns = a * kTurn, rest = fma(a, kTurn, -turns) + fma(a, kTurnRest, a_rest * kTurn);
     float s, c;
@@ -67,8 +73,9 @@ __device__ __forceinline__ void angles(const HeadsArgs &h, int64_t position, flo
     cs[i] = c * h.rope_scale;
     sn[i] = s * h.rope_scale;
   }
-  // the wave alone reads what it wrote
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+  // the wave alone reads what it wrote, and its LDS operations are done in their order: a wider fence
+  // would wait for the heads on their way
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
 
@@ -147,6 +154,7 @@ __global__ __launch_bounds__(kWaves *kWave) void heads_kernel(const HeadsArgs h,
   const Place at = place(h, lane % G);
   Weights w;
   load_weights(w, h, at);
+  const float freq = first_freq(h);
   const int64_t units = h.tokens * parts;
   for (int64_t unit = (int64_t)blockIdx.x * kWaves + wave; unit < units; unit += (int64_t)gridDim.x * kWaves) {
     const int64_t token = unit / parts;
@@ -168,7 +176,7 @@ __global__ __launch_bounds__(kWaves *kWave) void heads_kernel(const HeadsArgs h,
         xb[i] = load16(x + at.b);
       }
       if (step == first) {  // while the first heads are on their way
-        if (position >= 0) angles(h, position, cs[wave], sn[wave]);
+        if (position >= 0) angles(h, position, freq, cs[wave], sn[wave]);
         ang = lane_angles(cs[wave], sn[wave], at);
       }
 #pragma unroll
@@ -294,6 +302,7 @@ __global__ __launch_bounds__(kWaves *kWave, SUMS ? (Q == K ? 3 : 2) : 4) void he
   const Place at = place(h, lane % G);
   Weights w;
   load_weights(w, h, at);
+  const float freq = first_freq(h);
   float sq[SUMS ? 16 : 1], sk[SUMS ? 16 : 1];
   if constexpr (SUMS)
 #pragma unroll
@@ -312,7 +321,7 @@ __global__ __launch_bounds__(kWaves *kWave, SUMS ? (Q == K ? 3 : 2) : 4) void he
     const int64_t token = unit / parts;
     const int first = (int)(unit - token * parts) * per, last = min(first + per, steps);
     const bool pad = position < 0;
-    if (!pad) angles(h, position, cs[wave], sn[wave]);
+    if (!pad) angles(h, position, freq, cs[wave], sn[wave]);
     const Angles ang = lane_angles(cs[wave], sn[wave], at);
     // the next unit's first heads are loaded behind this one's last ones
     const int64_t unit2 = unit + stride < units ? unit + stride : unit, token2 = unit2 / parts;

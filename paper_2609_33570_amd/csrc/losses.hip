@@ -748,9 +748,13 @@ int groups_of(int64_t work, int64_t each) {
   return (int)(need < kMaxGroups ? need : kMaxGroups);
 }
 
-// One workgroup does all of a call whose steps would each be little more than a launch.
-bool small_call(const SequencesArgs &q, int64_t pairs) {
-  return q.tokens <= 8192 && q.sequences <= 1024 && q.sequences * pairs <= (1 << 16);
+// One workgroup does all of a call whose steps would each be little more than a launch.  Policy, one workgroup
+// against three launches (12.6 us up to some 8000 tokens): 64 tokens 7.6 us, 1024 7.3 to 8.9, 2048 10.6, 4096 16.
+// Preference (12.1): 1024 tokens 9.2, 3400 8.2, 4096 12 to 13.  With lists its 16 waves read them for a sequence
+// each: 98 sequences took 20 us, by launches 11.
+constexpr int kSmallPolicy = 2 * kSmall, kSmallPreference = 4 * kSmall;  // tokens
+bool small_call(const SequencesArgs &q, int64_t tokens, bool lists) {
+  return q.tokens > 0 && q.tokens <= tokens && q.sequences > 0 && q.sequences <= (lists ? kMaxWaves : kSmall);
 }
 
 size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
@@ -825,7 +829,7 @@ hipError_t launch_policy(const PolicyArgs &a, hipStream_t s) {
   Counts *counted = reinterpret_cast<Counts *>(a.part);
   double *part = a.part + kMaxGroups;
   if (a.seq.sequences == 0 && !a.stats) return hipSuccess;
-  if (a.seq.tokens > 0 && a.seq.sequences > 0 && small_call(a.seq, 0)) {
+  if (small_call(a.seq, kSmallPolicy, false)) {
     if (short_sequences(a.seq)) policy_small<8>(a, counted, part, s);
     else policy_small<64>(a, counted, part, s);
     return hipGetLastError();
@@ -858,7 +862,7 @@ size_t preference_workspace(PreferenceArgs &a, void *base) {
 
 hipError_t launch_preference(const PreferenceArgs &a, hipStream_t s) {
   if (a.seq.sequences == 0 && a.pairs == 0 && !a.stats) return hipSuccess;
-  if (a.seq.tokens > 0 && a.seq.sequences > 0 && small_call(a.seq, a.chosen ? a.pairs : 0)) {
+  if (small_call(a.seq, kSmallPreference, a.chosen != nullptr)) {
     if (short_sequences(a.seq)) hipLaunchKernelGGL(preference_small_kernel<8>, dim3(1), dim3(kSmall), 0, s, a, a.part);
     else hipLaunchKernelGGL(preference_small_kernel<64>, dim3(1), dim3(kSmall), 0, s, a, a.part);
     return hipGetLastError();
