@@ -396,9 +396,11 @@ int64_t segments_of(int64_t vocab, int f32) {
   return pieces == 0 ? 1 : (pieces + kSegment - 1) / kSegment;
 }
 
-// Few rows leave most of the chip idle: below four workgroups a CU their segments go to
-// workgroups of their own.
-bool split_rows(int64_t rows, int64_t segments) { return rows < 1024 && segments > 1; }
+// Few rows leave most of the chip idle and each takes its segments one after the other: then every segment is a
+// workgroup, for a second launch and the partials' way through memory.  bf16, whole and split, us: 1 x 32000 (two
+// segments) 6.4 and 9.1, x 65536 (four) 8.2 and 9.6, x 131072 (eight) 13.8 and 9.0; 64 x 65536 9.0 and 8.7, x
+// 131072 15.3 and 8.8; 256 x 131072 17.8 and 16.3; 512 x 65536 14.6 and 16.0, x 131072 25.7 and 26.2, x 262144 49 and 47.
+bool split_rows(int64_t rows, int64_t segments) { return rows <= 512 && segments > 4; }
 
 unsigned grid_of(int64_t units) { return (unsigned)(units < (1 << 22) ? units : (1 << 22)); }
 

@@ -208,7 +208,7 @@ template <int T, int W, bool DIFFERENCE, class Done>
 __device__ __forceinline__ void sum_sequences(const SequencesArgs &q, const float *x, const float *y, Place at, double (*lds)[kMaxSums],
                                               Done done) {
   constexpr int threads = W ? W : T, side = T / threads;
-  constexpr int kAhead = 4;  // tokens of a thread in flight
+  constexpr int kAhead = W == 0 && T > kThreads ? 8 : 4;  // tokens of a thread in flight
   const int mine = (int)threadIdx.x % threads;
   // Loads without branches, which would each wait for their own: what is not there is read from
   // x and not used, past the end the last token again.
@@ -458,16 +458,16 @@ __device__ __forceinline__ TokenLoss token_loss(const PolicyArgs &a, float delta
   return o;
 }
 
-template <int T, int V, bool BY_SEQUENCE>
-__device__ __forceinline__ void policy_tokens(const PolicyArgs &a, Place at, int chunks, const Counts *counted, int counters,
-                                              double *part, double (*lds)[kMaxSums]) {
+template <int T, int V>
+__device__ __forceinline__ void policy_tokens(const PolicyArgs &a, Place at, const Counts *counted, int counters, double *part,
+                                              double (*lds)[kMaxSums]) {
   double each = 0.0;  // 1 / N
   bool have = false;
   double sum[kPolicySums] = {};
   // what is not there is read from what is, and not used: branches around the loads would each wait
   const float *const from[4] = {a.logp, a.old, a.kl ? a.ref : a.logp, a.entropy ? a.entropy : a.logp};
   const float *const mean = a.sequence_ratio ? a.mean_delta : reinterpret_cast<const float *>(a.share);
-  each_tile<T, V, BY_SEQUENCE>(a.seq, at, chunks, [&](const Tokens<V> &k, int64_t first, int64_t end) {
+  each_tile<T, V, false>(a.seq, at, 0, [&](const Tokens<V> &k, int64_t first, int64_t end) {
     float in[4][V], adv[V], delta[V];
     double w64[V];
     const int64_t t = k.t;
@@ -550,10 +550,9 @@ __global__ __launch_bounds__(T) void policy_sequences_kernel(const PolicyArgs a,
   policy_sequences<T, W, RATIO>(a, Place{(int)blockIdx.x, (int)gridDim.x}, part, lds);
 }
 
-template <int T, bool BY_SEQUENCE>
-__global__ __launch_bounds__(T) void policy_tokens_kernel(const PolicyArgs a, int chunks, const Counts *counted, int counters, double *part) {
-  __shared__ double lds[T / kWave][kMaxSums];
-  policy_tokens<T, kVector, BY_SEQUENCE>(a, Place{(int)blockIdx.x, (int)gridDim.x}, chunks, counted, counters, part, lds);
+__global__ __launch_bounds__(kThreads) void policy_tokens_kernel(const PolicyArgs a, const Counts *counted, int counters, double *part) {
+  __shared__ double lds[kWaves][kMaxSums];
+  policy_tokens<kThreads, kVector>(a, Place{(int)blockIdx.x, (int)gridDim.x}, counted, counters, part, lds);
 }
 
 __global__ __launch_bounds__(kThreads) void policy_fold_kernel(const PolicyArgs a, const Counts *counted, int counters,
@@ -569,7 +568,7 @@ __global__ __launch_bounds__(kSmall) void policy_small_kernel(const PolicyArgs a
   const Place alone = {0, 1};
   policy_sequences<kSmall, W, RATIO>(a, alone, counted, lds);
   __syncthreads();
-  policy_tokens<kSmall, 1, false>(a, alone, 0, counted, 1, part, lds);
+  policy_tokens<kSmall, 1>(a, alone, counted, 1, part, lds);
   __syncthreads();
   if (a.stats) policy_fold<kSmall>(a, counted, 1, part, 1, lds);
 }
@@ -782,13 +781,15 @@ int sequence_groups(const SequencesArgs &q) {
   return groups_of(q.sequences, W ? T / W : 1);
 }
 
-// Calls f(T, W) as constants for the sequences' mean length.
+// Calls f(T, W) as constants for the sequences' mean length.  Policy passes over 2^19 tokens, us: length 64
+// 17.6 by 8 lanes, 18.9 by 64; 128 18.2 and 16.9; 256 16.1 by 64 lanes, 17.9 by 256 threads; 512 17.2 and 16.4; over
+// 2^20 tokens length 2048 20.6 by 256 threads, 21.4 by 1024; 4096 24.8 and 20.9.
 template <class F>
 void by_length(const SequencesArgs &q, F f) {
   const int64_t mean = q.sequences ? q.tokens / q.sequences : 0;
   if (mean <= 64) f(std::integral_constant<int, kThreads>(), std::integral_constant<int, 8>());
-  else if (mean <= 512) f(std::integral_constant<int, kThreads>(), std::integral_constant<int, 64>());
-  else if (mean <= 4096) f(std::integral_constant<int, kThreads>(), std::integral_constant<int, 0>());
+  else if (mean <= 384) f(std::integral_constant<int, kThreads>(), std::integral_constant<int, 64>());
+  else if (mean <= 2048) f(std::integral_constant<int, kThreads>(), std::integral_constant<int, 0>());
   else f(std::integral_constant<int, kSmall>(), std::integral_constant<int, 0>());
 }
 
@@ -808,7 +809,10 @@ void policy_small(const PolicyArgs &a, Counts *counted, double *part, hipStream_
   else hipLaunchKernelGGL((policy_small_kernel<W, false>), dim3(1), dim3(kSmall), 0, s, a, counted, part);
 }
 
-// Calls f(T, BY_SEQUENCE, workgroups, chunks) for a step over the tokens.
+// Calls f(T, BY_SEQUENCE, workgroups, chunks) for the preference loss's step over the tokens.  Passes over
+// 2^20 tokens, us: length 300 17.2 in tiles of all tokens, 18.3 by sequence; 600 17.3 and 16.1; 2048 15.7 and 13.8.
+// The policy loss, whose tokens take longer than the search for their sequences, takes tiles (600: 22.3 and 26.3;
+// 2048: 21.0 and 20.5; 8192: 20.8 and 22.1).
 constexpr int kSequenceThreads = 512;
 template <class F>
 void by_tiles(const SequencesArgs &q, F f) {
@@ -835,12 +839,9 @@ hipError_t launch_policy(const PolicyArgs &a, hipStream_t s) {
     return hipGetLastError();
   }
   const int counters = a.sequence_ratio ? policy_sums<true>(a, counted, s) : policy_sums<false>(a, counted, s);
-  int groups = 0;
-  if (a.seq.tokens > 0 && counters)
-    by_tiles(a.seq, [&](auto t, auto by_sequence, int g, int chunks) {
-      groups = g;
-      hipLaunchKernelGGL((policy_tokens_kernel<t(), by_sequence()>), dim3(g), dim3(t()), 0, s, a, chunks, counted, counters, part);
-    });
+  const int groups = counters ? groups_of(a.seq.tokens, kThreads * kVector) : 0;
+  if (groups)
+    hipLaunchKernelGGL(policy_tokens_kernel, dim3(groups), dim3(kThreads), 0, s, a, counted, counters, part);
   if (a.stats)
     hipLaunchKernelGGL(policy_fold_kernel, dim3(1), dim3(kThreads), 0, s, a, counted, counters, part, groups);
   return hipGetLastError();

@@ -78,7 +78,7 @@ def same(a, b):
     return [torch.equal(x, y) for x, y in zip(a, b)]
 
 
-@pytest.mark.parametrize("tokens,vocab", [(600, 5003), (1500, 40000), (12000, 700)])
+@pytest.mark.parametrize("tokens,vocab", [(600, 5003), (300, 100000), (1500, 40000), (12000, 700)])
 @pytest.mark.parametrize("own_workspace", [True, False])
 def test_graph_replays(hl, tokens, vocab, own_workspace):
     u = Update(hl, tokens, vocab)
@@ -104,7 +104,7 @@ def test_graph_replays(hl, tokens, vocab, own_workspace):
 def test_two_graphs_share_a_workspace(hl):
     """Replayed one after the other: each leaves nothing for the other to read."""
     a = Update(hl, 12000, 700, seed=1)
-    b = Update(hl, 900, 20001, seed=2, workspace=torch.empty(0))
+    b = Update(hl, 400, 90001, seed=2, workspace=torch.empty(0))
     shared = torch.full((max(a.need, b.need),), 0xFF, dtype=torch.uint8, device="cuda")
     a.ws = b.ws = shared
     graphs = []
@@ -127,7 +127,7 @@ def test_two_graphs_share_a_workspace(hl):
 
 
 def test_two_threads_two_streams(hl):
-    jobs = [Update(hl, 3000, 9001, seed=11), Update(hl, 700, 30001, seed=12)]
+    jobs = [Update(hl, 3000, 9001, seed=11), Update(hl, 200, 120001, seed=12)]
     want = []
     for u in jobs:
         u.run()
@@ -165,7 +165,7 @@ def test_an_explicit_stream_needs_a_workspace(hl):
 
 def test_a_torch_stream_is_followed(hl):
     """Calls under torch.cuda.stream run on it, with a workspace of its own."""
-    u = Update(hl, 900, 20001)
+    u = Update(hl, 450, 80001)
     u.run()
     want = u.outputs()
     u.q.zero_(), u.dlogits.zero_()

@@ -222,12 +222,13 @@ def test_confident_tokens_keep_their_precision(hl):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
-def test_a_rows_bits_do_not_depend_on_the_others(hl, dtype):
+@pytest.mark.parametrize("vocab", [40003, 100003])
+def test_a_rows_bits_do_not_depend_on_the_others(hl, dtype, vocab):
     """Split over workgroups or not, and wherever the row begins."""
-    z, t = logits(1200, 40003, dtype, 9)
-    zd, t = z.cuda(), t.abs().clamp(max=40002).cuda()
+    z, t = logits(1200, vocab, dtype, 9)
+    zd, t = z.cuda(), t.abs().clamp(max=vocab - 1).cuda()
     whole = forward(hl, zd, t, 1.0)
-    for a, b in ((0, 1), (3, 4), (1199, 1200), (5, 700)):
+    for a, b in ((0, 1), (3, 4), (1199, 1200), (5, 700), (7, 519), (7, 520)):
         some = forward(hl, zd[a:b], t[a:b], 1.0)
         assert all(torch.equal(some[k], whole[k][a:b]) for k in whole), (a, b)
 
