@@ -11,6 +11,10 @@
 // segments in order, then the waves are joined in order.  Where there are few rows a workgroup takes one segment and a
 // second kernel joins them in that same order, so that a row gives the same bits however many
 // rows the call has.
+//
+// Whole passes, bf16: 8192 x 131072 with entropy 322 to 332 us, 6.5 TB/s (loads kept in the caches 363), of which vector
+// instructions take 290, 9.4 a logit; one such row 9 us, two launches; backward with 30 % of the rows without a gradient
+// 600 us, 6.1 TB/s.  997 x 50021 f32 backward 67 us, 5.4 TB/s.
 #include "device_common.hpp"
 #include "hilore_internal.hpp"
 
@@ -22,7 +26,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kBatch = 4;                              // pieces of a lane in flight
-constexpr int kBatches = 2;                            // of a lane in a segment
+constexpr int kBatches = 2;                            // of a lane in a segment (8192 rows: 1 351 us, 2 331, 4 330; one row 8.7, 9.2, 9.0)
 constexpr int kSegment = kThreads * kBatch * kBatches; // pieces
 
 constexpr float kLowest = -3.402823466e38f;  // below every logit: exp2 of the way to it is 0

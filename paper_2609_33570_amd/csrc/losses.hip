@@ -1,9 +1,16 @@
 // Clipped policy loss and preference loss with their gradients, on gfx950.
 //
-// Small against the logits' passes (13 to 30 B a token): launches and the latencies inside them
-// count.  Three steps each: sums by sequence, then the tokens (policy) or the pairs (preference), then the fold of the
+//   policy      -A r, or -A times the bound that the log ratio is past;  + beta kl - bonus entropy;  times a weight
+//   preference  of h = L_chosen - L_rejected, L a sequence's sum of log-ratios:  softplus, hinge or square
+//
+// Small against the logits' passes (13 to 35 B a token): launches and the latencies inside them
+// bound both.  Three steps each: sums by sequence, then the tokens (policy) or the pairs (preference), then the
 // statistics or the tokens; every step is a launch, or all are one workgroup's phases where there is little to do.
 // Partial sums of a step's workgroups are added by the next step in a fixed order, in fp64.
+//
+// Whole passes: policy 1024 tokens 7.3 us, 2^20 packed tokens in 512 sequences 21 us (steps 6.8, 13.0 and 3.9 under a
+// trace; the bytes alone take 6); preference 16 x 211 tokens 8.2 us, 2^20 tokens in 768 sequences and 1152 listed
+// pairs 16 us (4.6, 5.3 and 6.4).
 #include "device_common.hpp"
 #include "hilore_internal.hpp"
 
