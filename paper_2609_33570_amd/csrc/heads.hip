@@ -56,6 +56,13 @@ __device__ __forceinline__ Place place(const HeadsArgs &h, int p) {
   return at;
 }
 
+// rsqrt(mean + eps), within 1 ulp of fp32 where the result is rounded to bf16.  The instruction takes a subnormal
+// operand for 0, which only an eps below the normal numbers lets through: the IEEE operations then.
+__device__ __forceinline__ float inverse_root(const HeadsArgs &h, float ss) {
+  const float v = ss * h.inv_dim + h.eps;
+  return h.eps >= 1.17549435e-38f ? __builtin_amdgcn_rsqf(v) : 1.0f / sqrtf(v);
+}
+
 // The token's cosines and sines times rope_scale, to the wave's part of LDS (freq: first_freq).  The angle in turns is a
 // product of two fp64 pairs (position * inv_freq and 1 / 2 pi with what their rounding leaves), so that
 // positions up to 2^53 turn as exactly as near ones: the fraction is rounded once, to 2^-25 of a turn.
@@ -195,8 +202,7 @@ __global__ __launch_bounds__(kWaves *kWave) void heads_kernel(const HeadsArgs h,
         for (int c = 0; c < 16; ++c) ss = fmaf(x[c], x[c], ss);
         ss = group_sum<G>(ss);
         if (key ? h.k.w != nullptr : h.q.w != nullptr) {
-          // within 1 ulp of fp32, where the result is rounded to bf16
-          const float r = __builtin_amdgcn_rsqf(ss * h.inv_dim + h.eps);
+          const float r = inverse_root(h, ss);
           float wv[16];
           unpack16(key ? w.k[0] : w.q[0], key ? w.k[1] : w.q[1], wv);
 #pragma unroll
@@ -367,7 +373,7 @@ __global__ __launch_bounds__(kWaves *kWave, SUMS ? (Q == K ? 3 : 2) : 4) void he
           // a head's lanes are all of one side, so all of them are here
           ss = group_sum<G>(ss);
           sx = group_sum<G>(sx);
-          const float r = __builtin_amdgcn_rsqf(ss * h.inv_dim + h.eps);
+          const float r = inverse_root(h, ss);
           const float along = r * (sx * h.inv_dim);
 #pragma unroll
           for (int c = 0; c < 16; ++c) x[c] *= r;

@@ -133,13 +133,22 @@ __device__ __forceinline__ void take(State &x, const u32x4 (&w)[kBatch], float c
   const State old = seen(x, m, c);
   float s = old.s, t = old.t;
 #pragma unroll
-  for (int p = 0; p < kBatch; ++p)
+  for (int p = 0; p < kBatch; ++p) {
+    // a piece's terms in pairs: a lane's sum of a segment has 11 roundings instead of 64
+    float e[E], u = 0.0f;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      const float d = c * (v[p][i] - m), e = __builtin_amdgcn_exp2f(d);
-      s += e;
-      if constexpr (ENTROPY) t = fmaf(e, fmaxf(d, kNoWay), t);
+      const float d = c * (v[p][i] - m);
+      e[i] = __builtin_amdgcn_exp2f(d);
+      if constexpr (ENTROPY) u = i == 0 ? e[i] * fmaxf(d, kNoWay) : fmaf(e[i], fmaxf(d, kNoWay), u);
     }
+#pragma unroll
+    for (int n = E / 2; n > 0; n /= 2)
+#pragma unroll
+      for (int i = 0; i < n; ++i) e[i] += e[i + n];
+    s += e[0];
+    if constexpr (ENTROPY) t += u;
+  }
   x = State{m, s, t};
 }
 

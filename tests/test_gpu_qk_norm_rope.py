@@ -171,14 +171,15 @@ CODES = [(None, None, 0), ("int8", "int8", 32), ("e4m3fn", None, 64), (None, "e4
          (None, "int8", 32), ("e4m3fn_cast", None, 0)]
 
 
-@pytest.mark.parametrize("code_q,code_k,block", CODES, ids=str)
-@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def saved_as(shape):
+    """The codes that the saved rows of a shape can have: blocks that divide them, none where none is read."""
+    _, hq, hk, dim, _, _, norm, _, _ = shape
+    return [c for c in CODES if (norm or c[:2] == (None, None)) and not (c[2] and (hq * dim % c[2] or hk * dim % c[2]))]
+
+
+@pytest.mark.parametrize("shape,code_q,code_k,block", [(s, *c) for s in SHAPES for c in saved_as(s)], ids=str)
 def test_backward(hl, shape, code_q, code_k, block):
     tokens, hq, hk, dim, rotated, pairs, norm, layout, pad = shape
-    if block and (hq * dim % block or hk * dim % block):
-        pytest.skip("blocks do not divide the rows")
-    if not norm and (code_q or code_k):
-        pytest.skip("nothing saved is read")
     g, rows, pos, w = inputs(shape, 23)
     freq = freqs(rotated)
     saved = [x.clone() for x in parts(rows[:, :(hq + hk) * dim], hq, hk, dim)]
@@ -282,3 +283,15 @@ def test_zero_rows_and_large_values(hl):
     out = torch.empty(2, 1, 64, dtype=torch.bfloat16, device="cuda")
     hl.hilore_qk_norm_rope(hl.qk_norm_rope_desc(q=x.cuda(), q_out=out, w_q=torch.ones(64, dtype=torch.bfloat16, device="cuda")))
     assert not out.any()
+
+
+def test_tiny_rows_without_eps(hl):
+    """Values whose squares are subnormal in fp32 (2^-70: a mean of 2^-140, 512 of the smallest steps, so exact), eps 0."""
+    x, go = torch.full((3, 64), 2.0 ** -70, dtype=torch.bfloat16), randn(gen(1), 3, 1, 64)
+    w, out, dx = torch.ones(64, dtype=torch.bfloat16), torch.empty(3, 1, 64, dtype=torch.bfloat16, device="cuda"), torch.empty(3, 64, dtype=torch.bfloat16, device="cuda")
+    hl.hilore_qk_norm_rope(hl.qk_norm_rope_desc(q=x.cuda(), q_out=out, w_q=w.cuda(), eps=0.0))
+    assert bool((out == 1.0).all())
+    hl.hilore_qk_norm_rope_bwd(hl.qk_norm_rope_bwd_desc(dq=go.cuda(), dq_in=dx, q=hl.unit_desc(x=x.cuda()), w_q=w.cuda(), eps=0.0))
+    pos, freq = torch.arange(3), torch.empty(0)
+    want, _, size, _ = R.heads_backward(x.double().reshape(3, 1, 64), w.double(), 0.0, pos, freq, False, go.double())
+    close(dx.unflatten(1, (1, 64)), want, size, 2.0 ** -17, "tiny")
