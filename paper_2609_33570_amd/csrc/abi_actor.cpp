@@ -56,7 +56,10 @@ bool apart(int64_t tokens, int heads, int dim, int64_t token_stride, int64_t hea
   if (heads <= 1) return token_stride >= dim;
   if (tokens <= 1) return head_stride >= dim;
   if (token_stride < dim || head_stride < dim) return false;
-  return token_stride >= (heads - 1) * head_stride + dim || head_stride >= (tokens - 1) * token_stride + dim;
+  // strides of up to 2^40 times 2^31 tokens: past 64 bits
+  const __int128 all_heads = (__int128)(heads - 1) * head_stride + dim;
+  const __int128 all_tokens = (__int128)(tokens - 1) * token_stride + dim;
+  return token_stride >= all_heads || head_stride >= all_tokens;
 }
 
 // Whether heads addressed by both strides lie as in rows `ld` apart.

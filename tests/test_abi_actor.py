@@ -33,7 +33,9 @@ def heads(lib, **kw):  # noqa: F811
     (ARG, dict(ld_q=248)), (ARG, dict(ld_k=120)), (ALIGN, dict(ld_q=260)), (ALIGN, dict(ld_k=132)),
     (ARG, dict(q_token_stride=0)), (ARG, dict(q_head_stride=0)), (ARG, dict(q_token_stride=-256)),
     (ARG, dict(q_token_stride=248)),   # the tokens' heads would overlap
-    (ARG, dict(q_token_stride=64, q_head_stride=248)), (ALIGN, dict(q_token_stride=260)), (ALIGN, dict(k_head_stride=68, k_token_stride=136)),
+    (ARG, dict(q_token_stride=64, q_head_stride=248)),
+    (ARG, dict(tokens=BIG - 1, q_token_stride=1 << 40, q_head_stride=1 << 40)),  # their product is past 64 bits
+    (ARG, dict(q_token_stride=1 << 41)), (ARG, dict(ld_q=1 << 41)), (ALIGN, dict(q_token_stride=260)), (ALIGN, dict(k_head_stride=68, k_token_stride=136)),
     (ARG, dict(q_out=FAKE, ld_q=320)),  # in place only with the rows' strides
     (ARG, dict(k_out=FAKE, k_token_stride=64, k_head_stride=256)),
     (ALIGN, dict(q=FAKE + 8)), (ALIGN, dict(k_out=FAKE + 8)), (ALIGN, dict(w_q=FAKE + 2)), (ALIGN, dict(positions=FAKE + 4)),
