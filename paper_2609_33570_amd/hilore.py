@@ -829,17 +829,35 @@ def _on_device(desc, *tensors):
     return _keeping(desc, *tensors)
 
 
-def _current(desc):
-    """The descriptor's address, refused where its tensors are not on the current device (whose
-    stream and memory the call uses)."""
-    device = getattr(desc, "_device", None)
-    if device is not None:
+def _device_now() -> int:
+    """Index of the current device (what torch.cuda.current_device() gives, without its check for a
+    first use: a descriptor's tensors are on a device already)."""
+    return _torch()._C._cuda_getDevice()
+
+
+_torch_module = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
         import torch
 
-        if device != torch.cuda.current_device():
-            raise ValueError(f"tensors on device {device}, the current one is "
-                             f"{torch.cuda.current_device()}")
-    return ctypes.byref(desc)
+        _torch_module = torch
+    return _torch_module
+
+
+def _current(desc, stream):
+    """(address of the descriptor, stream) of a call, refused where the descriptor's tensors are not on
+    the current device, whose stream and memory the call uses."""
+    device = getattr(desc, "_device", None)
+    if device is None:
+        return ctypes.byref(desc), _stream(stream)
+    now = _device_now()
+    if device != now:
+        raise ValueError(f"tensors on device {device}, the current one is {now}")
+    return (ctypes.byref(desc),
+            _torch()._C._cuda_getCurrentRawStream(now) if stream is None else int(stream))
 
 
 ROTATIONS = {"halves": 0, "pairs": 1}
@@ -922,7 +940,7 @@ def qk_norm_rope_desc(q, q_out, k=None, k_out=None, inv_freq=None, positions=Non
 
 def hilore_qk_norm_rope(desc: hilore_qk_norm_rope_desc, stream=None):
     """q_out, k_out = the heads of q and k normed and rotated by their tokens' positions."""
-    _check("hilore_qk_norm_rope", load().hilore_qk_norm_rope(_current(desc), _stream(stream)))
+    _check("hilore_qk_norm_rope", load().hilore_qk_norm_rope(*_current(desc, stream)))
 
 
 def qk_norm_rope_bwd_desc(dq, dk=None, dq_in=None, dk_in=None, q=None, k=None, inv_freq=None,
@@ -965,12 +983,12 @@ def hilore_qk_norm_rope_bwd(desc: hilore_qk_norm_rope_bwd_desc, code=0, block: i
     """Gradients of hilore_qk_norm_rope.  code and block are those of the L units among q and k (not
     read without one).  workspace: a device tensor of at least
     hilore_qk_norm_rope_bwd_workspace_bytes(desc) bytes, or None (taken from torch's allocator)."""
-    address = _current(desc)
+    address, on = _current(desc, stream)
     need = hilore_qk_norm_rope_bwd_workspace_bytes(desc) if workspace is None else 0
     wp, wb, _keep = _workspace(workspace, need, stream)
     _check("hilore_qk_norm_rope_bwd",
            load().hilore_qk_norm_rope_bwd(address, _code(code), int(block), 1 if accumulate else 0, wp,
-                                          wb, _stream(stream)))
+                                          wb, on))
 
 
 def _logits_of(t, name: str, rows: int, vocab: int):
@@ -1006,10 +1024,10 @@ def hilore_token_logprobs(desc: hilore_token_logprobs_desc, workspace=None, stre
     """Log-probabilities of the targets, entropies, maxima and log sums of the rows.  workspace: a
     device tensor of at least hilore_token_logprobs_workspace_bytes(desc) bytes, or None (taken from
     torch's allocator)."""
-    address = _current(desc)
+    address, on = _current(desc, stream)
     need = hilore_token_logprobs_workspace_bytes(desc) if workspace is None else 0
     wp, wb, _keep = _workspace(workspace, need, stream)
-    _check("hilore_token_logprobs", load().hilore_token_logprobs(address, wp, wb, _stream(stream)))
+    _check("hilore_token_logprobs", load().hilore_token_logprobs(address, wp, wb, on))
 
 
 def token_logprobs_bwd_desc(logits, targets, row_max, log_sum, dlogp, dlogits, entropy=None,
@@ -1032,8 +1050,7 @@ def token_logprobs_bwd_desc(logits, targets, row_max, log_sum, dlogp, dlogits, e
 
 def hilore_token_logprobs_bwd(desc: hilore_token_logprobs_bwd_desc, stream=None):
     """dlogits from the gradients of the targets' log-probabilities and of the entropies."""
-    _check("hilore_token_logprobs_bwd",
-           load().hilore_token_logprobs_bwd(_current(desc), _stream(stream)))
+    _check("hilore_token_logprobs_bwd", load().hilore_token_logprobs_bwd(*_current(desc, stream)))
 
 
 def _per_token(n: int, dtype: str, **tensors):
@@ -1090,10 +1107,10 @@ def hilore_policy_loss_workspace_bytes(desc: hilore_policy_loss_desc) -> int:
 def hilore_policy_loss(desc: hilore_policy_loss_desc, workspace=None, stream=None):
     """The clipped policy loss, its statistics and its gradients.  workspace: a device tensor of at
     least hilore_policy_loss_workspace_bytes(desc) bytes, or None (taken from torch's allocator)."""
-    address = _current(desc)
+    address, on = _current(desc, stream)
     need = hilore_policy_loss_workspace_bytes(desc) if workspace is None else 0
     wp, wb, _keep = _workspace(workspace, need, stream)
-    _check("hilore_policy_loss", load().hilore_policy_loss(address, wp, wb, _stream(stream)))
+    _check("hilore_policy_loss", load().hilore_policy_loss(address, wp, wb, on))
 
 
 def preference_loss_desc(logp, logp_ref=None, mask=None, offsets=None, sequences=None, chosen=None,
@@ -1131,7 +1148,7 @@ def hilore_preference_loss(desc: hilore_preference_loss_desc, workspace=None, st
     """The preference loss over pairs of sequences, its statistics and its gradient.  workspace: a
     device tensor of at least hilore_preference_loss_workspace_bytes(desc) bytes, or None (taken from
     torch's allocator)."""
-    address = _current(desc)
+    address, on = _current(desc, stream)
     need = hilore_preference_loss_workspace_bytes(desc) if workspace is None else 0
     wp, wb, _keep = _workspace(workspace, need, stream)
-    _check("hilore_preference_loss", load().hilore_preference_loss(address, wp, wb, _stream(stream)))
+    _check("hilore_preference_loss", load().hilore_preference_loss(address, wp, wb, on))

@@ -254,7 +254,7 @@ def test_another_device_is_refused(monkeypatch):
     with pytest.raises(ValueError, match="several devices"):
         E.token_logprobs_desc(OnDevice(0, 3, 9), OnDevice(1, 3, dtype=torch.int64))
     desc = E.token_logprobs_desc(OnDevice(1, 3, 9), OnDevice(1, 3, dtype=torch.int64))
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(E, "_device_now", lambda: 0)
     with pytest.raises(ValueError, match="device 1"):
         E.hilore_token_logprobs(desc)
 
