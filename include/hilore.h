@@ -822,7 +822,7 @@ hilore_status hilore_qk_norm_rope_bwd(const hilore_qk_norm_rope_bwd_desc *d, int
  * it is nearly all of S, logp = -log1p(the rest) keeps its relative precision.  A
  * row's bits do not depend on the other rows of the call.
  * workspace: device memory of at least hilore_token_logprobs_workspace_bytes(d) bytes (few
- * rows are split over workgroups; 0, and then NULL is allowed, for many), 16-byte aligned,
+ * long rows are split over workgroups; 0, and then NULL is allowed, for others), 16-byte aligned,
  * contents on entry irrelevant; calls sharing it must not overlap.
  * Limits: rows < 2^31, vocab < 2^28; vocab = 0 only with rows = 0.
  */

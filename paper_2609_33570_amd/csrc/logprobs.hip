@@ -9,8 +9,8 @@
 // Forward: one pass with the running maximum and sums of a softmax.  A row is cut into segments of
 // kSegment pieces of 16 bytes; a wave reduces its part of a segment over its lanes and joins the
 // segments in order, then the waves are joined in order.  Where there are few rows a workgroup takes one segment and a
-// second kernel joins them in that same order, so that a row gives the same bits however many
-// rows the call has.
+// second kernel joins them in that same order, or a larger workgroup takes four segments at a time, so that a row gives
+// the same bits however many rows the call has.
 //
 // Whole passes, bf16: 8192 x 131072 with entropy 322 to 332 us, 6.5 TB/s (loads kept in the caches 363), of which vector
 // instructions take 290, 9.4 a logit; one such row 9 us, two launches; backward with 30 % of the rows without a gradient
@@ -152,12 +152,12 @@ __device__ __forceinline__ void take(State &x, const u32x4 (&w)[kBatch], float c
   x = State{m, s, t};
 }
 
-// This wave's part of one segment of a row, the chosen token left out.
+// This wave's part of one segment of a row, the chosen token left out; `thread` of the kThreads that take it.
 template <bool F32, bool ENTROPY>
-__device__ __forceinline__ State segment_state(const void *row, int vocab, int segment, int target, float c) {
+__device__ __forceinline__ State segment_state(const void *row, int vocab, int segment, int target, float c, int thread) {
   constexpr int E = kPiece<F32>;
   const int pieces = vocab / E, chosen = target / E;
-  const int begin = segment * kSegment, mine = begin + (int)threadIdx.x;
+  const int begin = segment * kSegment, mine = begin + thread;
   State x = nothing();
   if (begin + kSegment <= pieces) {
 #pragma unroll
@@ -185,7 +185,7 @@ __device__ __forceinline__ State segment_state(const void *row, int vocab, int s
     }
   }
   if (begin + kSegment >= pieces) {  // the last segment: what is left behind the last whole piece
-    const int i = pieces * E + (int)threadIdx.x;
+    const int i = pieces * E + thread;
     if (i < vocab && i != target) {
       const float z = load_one<F32>(row, i), m = fmaxf(x.m, z);
       x = seen(x, m, c);
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobsArgs a
     const int place = target < a.vocab ? (int)target : (int)a.vocab;  // none is taken out past the end
     if (a.split) {
       if (target < 0) continue;
-      const State x = segment_state<F32, ENTROPY>(z, (int)a.vocab, (int)(unit - row * segments), place, c);
+      const State x = segment_state<F32, ENTROPY>(z, (int)a.vocab, (int)(unit - row * segments), place, c, (int)threadIdx.x);
       if ((threadIdx.x & 63) == 0) {
         float *o = a.part + (unit * kWaves + wave) * 4;
         o[0] = x.m;
@@ -250,7 +250,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobsArgs a
     const float zt = chosen_logit<F32>(a, row, target);
     State x = nothing();
     if (target >= 0)
-      for (int g = 0; g < segments; ++g) x = join(x, segment_state<F32, ENTROPY>(z, (int)a.vocab, g, place, c), c);
+      for (int g = 0; g < segments; ++g) x = join(x, segment_state<F32, ENTROPY>(z, (int)a.vocab, g, place, c, (int)threadIdx.x), c);
     if ((threadIdx.x & 63) == 0) lds[turn][wave] = x;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -261,33 +261,58 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobsArgs a
   }
 }
 
-// Joins the segments of split rows: four lanes a row, one for each wave that summed.
+// A row's state from those of its segments [segment][wave], `Get` of them: by four neighbouring lanes, one for each
+// wave that summed, all receiving it.
+template <class Get>
+__device__ __forceinline__ State join_segments(int segments, float c, Get get) {
+  State x = nothing();
+#pragma unroll 4
+  for (int g = 0; g < segments; ++g) x = join(x, get(g), c);
+  const int first = threadIdx.x & 63 & ~(kWaves - 1);
+  State all = {__shfl(x.m, first), __shfl(x.s, first), __shfl(x.t, first)};
+  for (int w = 1; w < kWaves; ++w) all = join(all, State{__shfl(x.m, first + w), __shfl(x.s, first + w), __shfl(x.t, first + w)}, c);
+  return all;
+}
+
+// Joins the segments of split rows, four lanes a row.
 template <bool F32>
 __global__ __launch_bounds__(kWave) void logprobs_join_kernel(const LogprobsArgs a, int segments) {
   const float c = a.scale * 1.4426950408889634f;
   const int64_t row = (int64_t)blockIdx.x * (kWave / kWaves) + threadIdx.x / kWaves;
+  const int64_t mine = row < a.rows ? row : a.rows - 1;  // past the last row the last one again, not written
   const int wave = threadIdx.x % kWaves;
-  State x = nothing();
-  int64_t target = -1;
-  float zt = 0.0f;
-  if (row < a.rows) {
-    // the segments of a row without a token hold anything, and are not used
-    const float *p = a.part + (row * segments * kWaves + wave) * 4;
-    target = a.targets[row];
-    zt = chosen_logit<F32>(a, row, target);
-#pragma unroll 4
-    for (int g = 0; g < segments; ++g) {
-      const float *q = p + (int64_t)g * kWaves * 4;
-      x = join(x, State{q[0], q[1], q[2]}, c);
+  // the segments of a row without a token hold anything, and are not used
+  const float *p = a.part + (mine * segments * kWaves + wave) * 4;
+  const int64_t target = a.targets[mine];
+  const float zt = chosen_logit<F32>(a, mine, target);
+  const State x = join_segments(segments, c, [&](int g) {
+    const float *q = p + (int64_t)g * kWaves * 4;
+    return State{q[0], q[1], q[2]};
+  });
+  if (wave == 0 && row < a.rows) finish(a, row, target, zt, x, c);
+}
+
+// A row by one workgroup, kSide segments side by side.
+constexpr int kSide = 4, kMaxWide = 16;  // segments at a time, and of a row
+
+template <bool F32, bool ENTROPY>
+__global__ __launch_bounds__(kSide *kThreads) void logprobs_wide_kernel(const LogprobsArgs a, int segments) {
+  __shared__ State lds[kMaxWide][kWaves];
+  const float c = a.scale * 1.4426950408889634f;
+  const int64_t row = blockIdx.x, target = a.targets[row];
+  const void *z = static_cast<const char *>(a.logits) + row * a.ld * (F32 ? 4 : 2);
+  const int place = target < a.vocab ? (int)target : (int)a.vocab;  // none is taken out past the end
+  const float zt = chosen_logit<F32>(a, row, target);
+  const int thread = threadIdx.x % kThreads, side = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+  if (target >= 0)
+    for (int g = side; g < segments; g += kSide) {
+      const State x = segment_state<F32, ENTROPY>(z, (int)a.vocab, g, place, c, thread);
+      if ((threadIdx.x & 63) == 0) lds[g][thread >> 6] = x;
     }
-  }
-  State all = x;
-  for (int w = 1; w < kWaves; ++w) {
-    const int from = (threadIdx.x & ~(kWaves - 1)) + w;
-    const State y = {__shfl(x.m, from), __shfl(x.s, from), __shfl(x.t, from)};
-    all = join(all, y, c);
-  }
-  if (wave == 0 && row < a.rows) finish(a, row, target, zt, all, c);
+  __syncthreads();
+  if (threadIdx.x >= kWaves) return;
+  const State x = join_segments(target >= 0 ? segments : 0, c, [&](int g) { return lds[g][threadIdx.x]; });
+  if (threadIdx.x == 0) finish(a, row, target, zt, x, c);
 }
 
 // --------------------------------------------------------------- backward --
@@ -409,11 +434,19 @@ int64_t segments_of(int64_t vocab, int f32) {
   return pieces == 0 ? 1 : (pieces + kSegment - 1) / kSegment;
 }
 
-// Few rows leave most of the chip idle and each takes its segments one after the other: then every segment is a
-// workgroup, for a second launch and the partials' way through memory.  bf16, whole and split, us: 1 x 32000 (two
-// segments) 6.4 and 9.1, x 65536 (four) 8.2 and 9.6, x 131072 (eight) 13.8 and 9.0; 64 x 65536 9.0 and 8.7, x
-// 131072 15.3 and 8.8; 256 x 131072 17.8 and 16.3; 512 x 65536 14.6 and 16.0, x 131072 25.7 and 26.2, x 262144 49 and 47.
-bool split_rows(int64_t rows, int64_t segments) { return rows <= 512 && segments > 4; }
+// Few rows leave most of the chip idle, and a workgroup takes its segments one after the other.  Two ways out.  Wide:
+// four times the waves take four segments at a time, one workgroup a row and so no more rows than CUs.  Split: every
+// segment is a workgroup, for a second launch and the partials' way through memory.  bf16, us, whole, wide and split:
+//   1 x 32000 (two segments) 6.1, 5.7, 8.2     1 x 65536 (four) 8.2, 6.7, 8.8      1 x 131072 (eight) 13.9, 10.9, 8.6
+//   64 x 65536 9.3, 7.4, 8.0                   64 x 131072 15.5, 12.0, 8.3         128 x 131072 16.6, 12.6, 11.2
+//   200 x 65536 10.0, 7.6, 10.3                200 x 131072 17.1, 12.9, 14.7       256 x 262144 (16) 31.7, 25.8, 28.1
+//   300 x 65536 13.9, 12.6, 11.7               300 x 131072 24.8, 22.1, 18.8       512 x 131072 26.4, 25.3, 27.6
+// f32: 16 x 32000 (four) 8.3, 5.7, 8.1, 200 x 131072 (16) 24.7, 19.2, 21.1.
+bool wide_rows(int64_t rows, int64_t segments) {
+  return rows <= 256 && segments > 1 && segments <= kMaxWide && (rows > 128 || segments <= 4);
+}
+
+bool split_rows(int64_t rows, int64_t segments) { return rows <= 512 && segments > 4 && !wide_rows(rows, segments); }
 
 unsigned grid_of(int64_t units) { return (unsigned)(units < (1 << 22) ? units : (1 << 22)); }
 
@@ -428,6 +461,17 @@ hipError_t launch_logprobs(const LogprobsArgs &args, hipStream_t s) {
   if (args.rows == 0) return hipSuccess;
   LogprobsArgs a = args;
   const int64_t segments = segments_of(a.vocab, a.f32);
+  if (wide_rows(a.rows, segments)) {
+    const dim3 grid((unsigned)a.rows), block(kSide * kThreads);
+    if (a.f32) {
+      if (a.entropy) hipLaunchKernelGGL((logprobs_wide_kernel<true, true>), grid, block, 0, s, a, (int)segments);
+      else hipLaunchKernelGGL((logprobs_wide_kernel<true, false>), grid, block, 0, s, a, (int)segments);
+    } else {
+      if (a.entropy) hipLaunchKernelGGL((logprobs_wide_kernel<false, true>), grid, block, 0, s, a, (int)segments);
+      else hipLaunchKernelGGL((logprobs_wide_kernel<false, false>), grid, block, 0, s, a, (int)segments);
+    }
+    return hipGetLastError();
+  }
   a.split = split_rows(a.rows, segments) ? 1 : 0;
   const dim3 grid(grid_of(a.split ? a.rows * segments : a.rows)), block(kThreads);
   if (a.f32) {

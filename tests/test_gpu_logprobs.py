@@ -233,6 +233,20 @@ def test_a_rows_bits_do_not_depend_on_the_others(hl, dtype, vocab):
         assert all(torch.equal(some[k], whole[k][a:b]) for k in whole), (a, b)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [16387, 32773, 65531, 65544, 100003, 262143])
+def test_counts_of_rows_about_the_chip(hl, dtype, vocab):
+    """One workgroup a row, larger ones, and a row split over several: right, and the same bits."""
+    z, t = logits(260, vocab, dtype, 10)
+    zd, td = z.cuda(), t.cuda()
+    whole = forward(hl, zd.repeat(2, 1)[:515], td.repeat(2)[:515], 1.0)
+    for rows in (1, 30, 128, 129, 200, 256, 257):
+        some = forward(hl, zd[:rows], td[:rows], 1.0)
+        assert all(torch.equal(some[k], whole[k][:rows]) for k in whole), rows
+    few = forward(hl, zd[:60], td[:60], 1.0)
+    check_forward(few, z[:60], t[:60], 1.0)
+
+
 def test_shifted_slices(hl):
     """Targets and logits one row apart, as a causal model has them: addresses between 16-byte steps."""
     z, _ = logits(30, 4001, BF16, 12)
