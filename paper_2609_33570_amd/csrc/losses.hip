@@ -180,7 +180,7 @@ __device__ __forceinline__ void begins_before(const SequencesArgs &q, int t0, in
     bool read[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      step[k] = (int)((uint32_t)(n[k] + kWave - 1) / kWave);
+      step[k] = (int)(((uint32_t)n[k] + kWave - 1) / kWave);
       const int64_t i = (int64_t)(lane + 1) * step[k] - 1;
       read[k] = i < n[k];
       begin[k] = offset(q, read[k] ? lo[k] + (int)i : 0);
@@ -230,7 +230,7 @@ __device__ __forceinline__ void sum_sequences(const SequencesArgs &q, const floa
     if (live) bounds(q, s, begin, end);
     uint32_t count = 0;
     double sum[1] = {0.0};
-    for (int64_t t = begin + mine; t < end; t += kAhead * threads) {
+    for (int64_t t = (int64_t)begin + mine; t < end; t += kAhead * threads) {
       uint8_t m[kAhead];
       float u[kAhead], v[kAhead];
 #pragma unroll

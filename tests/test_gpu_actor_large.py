@@ -135,3 +135,34 @@ def test_preference_lists_of_many_pairs(hl):
     hl.hilore_preference_loss(hl.preference_loss_desc(new, dlogp=a))
     hl.hilore_preference_loss(hl.preference_loss_desc(new, chosen=2 * order, rejected=2 * order + 1, dlogp=b))
     assert torch.allclose(a, b, rtol=2.0 ** -23, atol=0)
+
+
+@pytest.mark.parametrize("length", [40, 256, 1024, 4096])
+def test_losses_of_the_most_tokens(hl, length):
+    """2^31 - 1 tokens, whose last sequences begin fewer tokens before 2^31 than a workgroup has threads."""
+    n, tail = (1 << 31) - 1, 600
+    g = torch.Generator(device="cuda").manual_seed(7)
+    ends = torch.tensor([n - tail, n - 300, n - 3, n], device="cuda")
+    offsets = torch.cat((torch.arange(0, n - tail, length, device="cuda"), ends))
+    sequences = offsets.numel() - 1
+    new, old = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    new[-tail:], old[-tail:] = (torch.randn(tail, generator=g, device="cuda") for _ in range(2))
+    d, stats = torch.full((n,), 9.0, device="cuda"), torch.empty(8, device="cuda")
+    adv = torch.ones(sequences, device="cuda")
+    few, part = slice(n - tail, n), torch.full((tail,), 9.0, device="cuda")
+    kw = dict(ratio="sequence", mean="sequences", n_norm=1000.0, clip_high=5.0)
+    hl.hilore_policy_loss(hl.policy_loss_desc(new, old, adv, offsets=offsets, dlogp=d, stats=stats, **kw))
+    hl.hilore_policy_loss(hl.policy_loss_desc(new[few], old[few], adv[:3], offsets=ends - (n - tail), dlogp=part, **kw))
+    # means and weights of one call against the other's: a rounding each of the weight, the mean, exp (2) and the product
+    assert torch.allclose(d[few], part, rtol=2.0 ** -21, atol=0)
+    assert float(stats[6]) == 2.0 ** 31 and float(stats[7]) == float(torch.tensor(float(sequences)))
+    # equal ratios of 1 in all other sequences: weight 1 / (1000 length) each
+    assert float(d[0]) == float(d[length * 5 + 3]) == pytest.approx(-1e-3 / length, rel=2.0 ** -22)
+    rewards, six = torch.empty(sequences, device="cuda"), torch.empty(6, device="cuda")
+    d.fill_(9.0)
+    hl.hilore_preference_loss(hl.preference_loss_desc(new, old, offsets=offsets, beta=1.0, dlogp=d, rewards=rewards, stats=six))
+    x = (new[few] - old[few]).double()
+    want = torch.stack([x[:300].sum(), x[300:597].sum(), x[597:].sum()])
+    assert ((rewards[-3:].double() - want).abs() <= 2.0 ** -23 * want.abs() + 1e-12).all()
+    assert not rewards[:-3].any() and float(six[5]) == float(torch.tensor(float(sequences // 2)))
+    assert not (d[few] == 9.0).any()
