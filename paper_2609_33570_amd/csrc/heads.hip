@@ -453,13 +453,15 @@ int lanes_of(int dim) {
 
 // Waves that share a token's heads: more than one until 4096 waves are at work.  28 + 4 heads of 128, us with one
 // wave a token and with several: 64 tokens 6.0 and 5.1, 512 6.3 and 5.0, 2048 7.1 and 6.6, 4096 11.0 (16 waves a
-// token 15.0); backward 64 tokens 12.4 and 9.9, 512 14.9 and 12.0.
+// token 15.0); backward 64 tokens 12.4 and 9.9, 512 14.9 and 12.0.  None of them is without a head: the backward loads
+// the next unit's first heads behind a unit's last ones.
 int parts_of(int64_t tokens, int heads, int dim) {
   const int side = kWave / lanes_of(dim);
   const int steps = (heads + side - 1) / side;
   int parts = 1;
   while (parts < steps && tokens * parts < 4096) parts *= 2;
-  return parts < steps ? parts : steps;
+  const int per = (steps + parts - 1) / parts;  // of a wave
+  return (steps + per - 1) / per;
 }
 
 template <int G>

@@ -52,6 +52,24 @@ def test_heads_of_many_tokens(hl):
         assert torch.equal(part, out[a:a + 300]) and torch.equal(dpart, dx[a:a + 300])
 
 
+@pytest.mark.parametrize("dim,heads", [(512, 4200), (256, 8206)])
+def test_heads_backward_of_thousands_of_heads(hl, dim, heads):
+    """Three tokens whose heads are more than waves take: each head's gradient as a call with fewer heads has it."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x, go = (torch.randn(3, heads, dim, generator=g, device="cuda").bfloat16() for _ in range(2))
+    w = torch.randn(dim, generator=g, device="cuda").bfloat16()
+    dx, dw = torch.full_like(x, 9.0), torch.empty(dim, device="cuda")
+    hl.hilore_qk_norm_rope_bwd(hl.qk_norm_rope_bwd_desc(dq=go, dq_in=dx.view(3, -1), q=hl.unit_desc(x=x.view(3, -1)), w_q=w, dw_q=dw))
+    for a in range(0, heads, 700):
+        xs, gs = x[:, a:a + 700].contiguous(), go[:, a:a + 700].contiguous()
+        part, dpart = torch.full_like(xs, 9.0), torch.empty(dim, device="cuda")
+        hl.hilore_qk_norm_rope_bwd(hl.qk_norm_rope_bwd_desc(dq=gs, dq_in=part.view(3, -1), q=hl.unit_desc(x=xs.view(3, -1)), w_q=w, dw_q=dpart))
+        assert torch.equal(part, dx[:, a:a + 700]), a
+    terms = go.double() * x.double() * torch.rsqrt(x.double().square().mean(-1, keepdim=True) + 1e-6)
+    # fewer than 100 roundings on a term's way into its sum, and two units in the last place of the root
+    assert ((dw.double() - terms.sum((0, 1))).abs() <= 104 * 2.0 ** -24 * terms.abs().sum((0, 1))).all()
+
+
 def test_logprobs_of_many_rows(hl):
     n = (1 << 22) + 300  # more than one row to each workgroup of the largest grid
     g = torch.Generator(device="cuda").manual_seed(3)
