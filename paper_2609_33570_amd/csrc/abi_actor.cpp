@@ -180,10 +180,11 @@ hilore::HeadSide bwd_side(const hilore_unit_desc &saved, const uint16_t *w, cons
   return s;
 }
 
+// Of the power of two that a block is; 0 for what stands there where no unit has blocks.
 int log2_of(int block) {
   int l = 0;
-  while ((1 << l) < block) ++l;
-  return l;
+  while (l < 30 && (1 << l) < block) ++l;
+  return (1 << l) == block ? l : 0;
 }
 
 // --------------------------------------------------------------- logprobs --

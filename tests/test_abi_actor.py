@@ -155,6 +155,11 @@ def test_preference(lib, want, kw):  # noqa: F811
     assert lib.hilore_preference_loss(ctypes.byref(d), ws, ws_bytes, None) == want
 
 
+@pytest.mark.parametrize("block", [-1, 0, 3, 1 << 30, (1 << 30) + 1, (1 << 31) - 1])
+def test_heads_bwd_without_codes_takes_any_block(lib, block):  # noqa: F811
+    assert heads_bwd(lib, block=block, tokens=0, dw_q=None, dw_k=None) == OK
+
+
 def test_null_descriptors(lib):  # noqa: F811
     assert lib.hilore_qk_norm_rope(None, None) == ARG
     assert lib.hilore_qk_norm_rope_bwd(None, 0, 0, 0, None, 0, None) == ARG
