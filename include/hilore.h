@@ -814,7 +814,7 @@ hilore_status hilore_qk_norm_rope_bwd(const hilore_qk_norm_rope_bwd_desc *d, int
  *            value: rows may begin anywhere)
  *   targets  i64 [rows].  A negative target is a row without a token: it is not read and
  *            its outputs are 0.  A target >= vocab gives logp NaN
- *   scale    1 / temperature, positive
+ *   scale    1 / temperature, from 2^-126 to 2^127
  * Outputs f32 [rows], each may be NULL: logp, entropy, row_max = m and log_sum = log S
  * (which the backward takes: m and log S apart keep what their sum would round away).
  * Columns of -inf have p = 0; a row of nothing else, or with +inf or NaN, gives NaN.

@@ -188,9 +188,10 @@ int log2_of(int block) {
 }
 
 // --------------------------------------------------------------- logprobs --
+// scale log2(e) has to be finite.
 hilore_status check_logits(int64_t rows, int64_t vocab, float scale) {
   if (rows < 0 || vocab < 0 || (rows > 0 && vocab == 0)) return HILORE_ERR_INVALID_ARG;
-  if (!std::isfinite(scale) || !(scale >= FLT_MIN)) return HILORE_ERR_INVALID_ARG;
+  if (!(scale >= FLT_MIN) || !(scale <= 0x1p127f)) return HILORE_ERR_INVALID_ARG;
   if (rows >= kMaxRows || vocab >= (int64_t(1) << 28)) return HILORE_ERR_UNSUPPORTED;
   return HILORE_OK;
 }

@@ -155,6 +155,14 @@ def test_preference(lib, want, kw):  # noqa: F811
     assert lib.hilore_preference_loss(ctypes.byref(d), ws, ws_bytes, None) == want
 
 
+@pytest.mark.parametrize("scale,want", [(2.0 ** -126, OK), (2.0 ** 127, OK), (1.01 * 2.0 ** 127, ARG), (3.4e38, ARG), (2.0 ** -127, ARG)])
+def test_logprobs_scales(lib, scale, want):  # noqa: F811
+    for name, ws in (("token_logprobs", (None, 0)), ("token_logprobs_bwd", ())):
+        d = getattr(E, f"hilore_{name}_desc")()
+        d.vocab, d.ld, d.scale = 8, 8, scale
+        assert getattr(lib, f"hilore_{name}")(ctypes.byref(d), *ws, None) == want
+
+
 @pytest.mark.parametrize("block", [-1, 0, 3, 1 << 30, (1 << 30) + 1, (1 << 31) - 1])
 def test_heads_bwd_without_codes_takes_any_block(lib, block):  # noqa: F811
     assert heads_bwd(lib, block=block, tokens=0, dw_q=None, dw_k=None) == OK

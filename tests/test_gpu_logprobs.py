@@ -258,6 +258,21 @@ def test_shifted_slices(hl):
     check_forward(o, z[1:], ids[:-1], 1.0)
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -126, 2.0 ** 127])
+def test_ends_of_the_scales(hl, scale):
+    """The distribution is uniform, or the largest logit's alone."""
+    z, t = torch.tensor([[1.0, 2.0, 3.0]] * 2, device="cuda"), torch.tensor([2, 1], device="cuda")
+    o, d = forward(hl, z, t, scale), torch.full((2, 3), 5.0, device="cuda")
+    one = torch.ones(2, device="cuda")
+    hl.hilore_token_logprobs_bwd(hl.token_logprobs_bwd_desc(z, t, o["row_max"], o["log_sum"], one, d, entropy=o["entropy"], dentropy=one, scale=scale))
+    if scale > 1.0:
+        assert o["logp"].tolist() == [0.0, -scale] and o["entropy"].tolist() == [0.0, 0.0]
+        assert d.tolist() == [[0.0, 0.0, 0.0], [0.0, scale, -scale]]
+    else:
+        assert torch.allclose(o["logp"], -torch.log(3 * one), rtol=2.0 ** -21) and torch.allclose(o["entropy"], torch.log(3 * one), rtol=2.0 ** -21)
+        assert (d.abs() <= scale).all()
+
+
 def test_no_rows(hl):
     z = torch.empty(0, 100, dtype=BF16, device="cuda")
     t, e = torch.empty(0, dtype=torch.int64, device="cuda"), torch.empty(0, device="cuda")
