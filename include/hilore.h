@@ -891,9 +891,9 @@ typedef enum hilore_mean {
  * Clipped policy loss with a KL term and an entropy bonus (Sec. 3.1 Eq. grpo-objective and
  * its usual variants): its value, its statistics and its gradient to each log-probability
  * and entropy.  For a valid token with advantage A and log ratio delta:
- *   chi    = delta <= log1p(clip_high) where A >= 0, else delta >= log1p(-clip_low)
- *            (thresholds rounded to fp32, as in hilore_grpo_coeffs) and, with dual_clip > 0
- *            and A < 0, delta <= log(dual_clip); dual_clip is 0 or above 1
+ *   chi    = not (delta > log1p(clip_high) where A >= 0, delta < log1p(-clip_low) where A < 0;
+ *            thresholds rounded to fp32, as in hilore_grpo_coeffs) and, with dual_clip > 0
+ *            and A < 0, not delta > log(dual_clip); dual_clip is 0 or above 1.  So a NaN stays
  *   policy = -A r where chi holds, r = exp(delta), else -A times the bound that delta is past
  *            (1 + clip_high, 1 - clip_low or dual_clip); 0 where A = 0
  *   loss   = sum over valid tokens of weight * (policy + beta * kl - entropy_weight * entropy)

@@ -434,7 +434,7 @@ struct TokenLoss {
 __device__ __forceinline__ TokenLoss token_loss(const PolicyArgs &a, float delta, float adv, float x, float entropy) {
   TokenLoss o;
   o.ratio = expf(delta);
-  bool chi = adv >= 0.0f ? delta <= a.log_high : delta >= a.log_low;
+  bool chi = !(adv >= 0.0f ? delta > a.log_high : adv < 0.0f && delta < a.log_low);  // no bound hides a NaN
   float bound = adv >= 0.0f ? a.bound_high : a.bound_low;
   if (a.dual > 0.0f && adv < 0.0f && delta > a.log_dual) {
     chi = false;

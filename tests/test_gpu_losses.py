@@ -117,6 +117,30 @@ def test_policy_advantage_of_each_token(hl, kind):
     check_policy(got, R.policy_loss(new, old, adv, s, None, None, mask, offsets, mean="sequences"), n, offsets)
 
 
+@pytest.mark.parametrize("n", [600, 30000])
+@pytest.mark.parametrize("ratio", ["token", "sequence"])
+def test_policy_hides_no_nan(hl, n, ratio):
+    """A valid token whose ratio is NaN, a bound or not, and an advantage that is."""
+    s = 6
+    _, new, old, _, _ = batch(n, 30)
+    adv = torch.tensor([1.0, -1.0, 0.0, math.nan, 0.5, -0.5])
+    length = n // s
+    new[3], old[length + 5] = math.nan, -math.inf
+    new[length + 5] = -math.inf
+    new[2 * length + 1] = math.nan  # no advantage: no policy term
+    mask = torch.ones(n, dtype=torch.uint8)
+    mask[4 * length + 2], new[4 * length + 2] = 0, math.nan
+    got = run_policy(hl, n, s, None, mask, new, old, adv, ratio=ratio)
+    bad = torch.zeros(n, dtype=torch.bool)
+    bad[3 * length:4 * length] = True
+    bad[3] = bad[length + 5] = True
+    if ratio == "sequence":
+        bad[:2 * length] = True
+    for k in ("dlogp", "token_loss"):
+        assert torch.equal(torch.isnan(got[k].cpu()), bad), k
+    assert math.isnan(float(got["stats"][0])) and math.isnan(float(got["stats"][1]))
+
+
 def test_policy_is_the_update_coefficient(hl):
     """With the symmetric clip, K3 and the tokens' mean, dlogp is what hilore_grpo_coeffs gives."""
     P, G, T = 3, 8, 40
