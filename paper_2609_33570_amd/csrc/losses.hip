@@ -341,7 +341,7 @@ __device__ __forceinline__ Tokens<V> tokens_of(const SequencesArgs &q, int s, in
   return k;
 }
 
-// A wave's tokens from `first` on (first < q.tokens), of whatever sequences.
+// A wave's tokens from `first` on (first < q.tokens), of whatever sequences (there is one at least: its ends are read).
 template <int V>
 __device__ __forceinline__ Tokens<V> tokens_at(const SequencesArgs &q, int64_t first) {
   Tokens<V> k;
@@ -704,7 +704,7 @@ __device__ __forceinline__ void preference_tokens(const PreferenceArgs &a, Place
     for (int k = 1; k < kPairSums; ++k) a.stats[k - 1] = (float)(v[k] / norm);
     a.stats[5] = (float)v[0];
   }
-  if (!a.dlogp) return;
+  if (!a.dlogp || a.seq.sequences == 0) return;  // tokens of no sequence are left as they were
   const double each = 1.0 / norm;
   each_tile<T, V, BY_SEQUENCE>(a.seq, at, chunks, [&](const Tokens<V> &k, int64_t, int64_t) {
     double slope[V];
