@@ -1077,24 +1077,33 @@ def policy_loss_desc(logp, logp_old, adv, logp_ref=None, entropy=None, mask=None
                      sequences=None, clip_low: float = _d.CLIP_EPS, clip_high: float = _d.CLIP_EPS,
                      dual_clip: float = 0.0, beta: float = 0.0, entropy_weight: float = 0.0, kl: int = 0,
                      ratio="token", mean="tokens", n_norm: float = 0.0, dlogp=None, dentropy=None,
-                     token_loss=None, flags=None, stats=None) -> hilore_policy_loss_desc:
+                     token_loss=None, flags=None, stats=None,
+                     adv_per_token: Optional[bool] = None) -> hilore_policy_loss_desc:
     """Descriptor of hilore_policy_loss: per-token tensors f32 of one size (any shape, dense), mask
     and flags u8 or bool, adv f32 with one value a sequence or a token, offsets i64 [sequences + 1]
     of packed sequences (None: `sequences` rows of equal length, or logp's rows), kl 0 (none) or 1, 2, 3 for
-    the estimators K1 to K3, stats f32 [8]."""
+    the estimators K1 to K3, stats f32 [8].  adv_per_token: which of the two adv holds; None: its
+    size tells, and the call is refused where there are as many packed sequences (some may be empty) as tokens."""
     n = int(logp.numel())
     count = _sequences(logp, offsets, sequences)
     _per_token(n, "float32", logp=logp, logp_old=logp_old, logp_ref=logp_ref, entropy=entropy,
                dlogp=dlogp, dentropy=dentropy, token_loss=token_loss)
     _per_token(n, "uint8|bool", mask=mask, flags=flags)
-    if _typed(adv, "adv", "float32").numel() not in (count, n):
-        raise ValueError(f"adv needs {count} or {n} elements, got {adv.numel()}")
+    ratio = _choice(ratio, RATIOS, "ratio")
+    sizes = (count, n) if adv_per_token is None else (n if adv_per_token else count,)
+    if _typed(adv, "adv", "float32").numel() not in sizes:
+        raise ValueError(f"adv needs {' or '.join(map(str, sizes))} elements, got {adv.numel()}")
+    if adv_per_token is None:
+        # one ratio a sequence takes one advantage a sequence; rows of one token are their sequences
+        if count == n > 0 and offsets is not None and ratio == RATIOS["token"]:
+            raise ValueError(f"{n} packed sequences and {n} tokens: adv_per_token must say which adv holds")
+        adv_per_token = adv.numel() != count
     _sized(_typed(stats, "stats", "float32"), "stats", 8)
     desc = hilore_policy_loss_desc(_p(logp), _p(logp_old), _p(logp_ref), _p(entropy), _p(adv), _p(mask),
                                    _p(offsets), _p(dlogp), _p(dentropy), _p(token_loss), _p(flags), _p(stats),
                                    n, count, float(n_norm), float(clip_low), float(clip_high),
                                    float(dual_clip), float(beta), float(entropy_weight),
-                                   0 if adv.numel() == count else 1, _choice(ratio, RATIOS, "ratio"),
+                                   1 if adv_per_token else 0, ratio,
                                    int(kl), _choice(mean, MEANS, "mean"))
     return _on_device(desc, logp, logp_old, logp_ref, entropy, adv, mask, offsets, dlogp, dentropy,
                       token_loss, flags, stats)
