@@ -965,7 +965,8 @@ typedef enum hilore_preference {
  * margin of a pair:
  *   loss = (1 / N) sum over pairs of loss(h);   dlogp of a valid token of sequence i =
  *   (1 / N) (sum of loss'(h) over pairs that choose i - sum over pairs that reject i),
- *   over n_i with length_mean
+ *   over n_i with length_mean.  An L of -inf (a token that cannot be) gives an infinite h, with
+ *   the losses' limits: logistic without smoothing 0 at +inf
  * Sequences, mask and n_tokens as for hilore_policy_loss.
  *   chosen, rejected  i32 [pairs] sequence numbers, or both NULL: pair p is sequences 2p and
  *            2p + 1 (pairs = sequences / 2).  A sequence may be in many pairs, or in none

@@ -612,8 +612,10 @@ __device__ __forceinline__ Pair pair_loss(const PreferenceArgs &a, int64_t win, 
   const double y = beta * p.h;
   if (a.loss == 0) {
     const double eps = a.smoothing, tail = log1p(exp(-fabs(y)));
-    // softplus(-y) and softplus(y); their slopes are -sigmoid(-y) and sigmoid(y)
-    p.loss = (1.0 - eps) * (fmax(-y, 0.0) + tail) + eps * (fmax(y, 0.0) + tail);
+    // softplus(-y) and softplus(y); their slopes are -sigmoid(-y) and sigmoid(y).  An infinite one of weight 0 adds
+    // nothing: y is +inf where a token of the rejected has the log-probability -inf
+    p.loss = (1.0 - eps) * (fmax(-y, 0.0) + tail);
+    if (eps > 0.0) p.loss += eps * (fmax(y, 0.0) + tail);
     p.slope = beta * (eps / (1.0 + exp(-y)) - (1.0 - eps) / (1.0 + exp(y)));
   } else if (a.loss == 1) {
     p.loss = y < 1.0 ? 1.0 - y : 0.0;
