@@ -426,6 +426,23 @@ __device__ __forceinline__ void policy_sequences(const PolicyArgs &a, Place at, 
 
 constexpr int kPolicySums = 6;  // policy, kl, entropy, loss, clipped, ratio
 
+// exp(-x) - 1 + x, whose first terms cancel near 0, where a policy is beside its reference: x^2 / 2 times its series
+// 2 (-x)^k / (k + 2)! below 1 (cut off at 2^-27), the sum from expm1 beyond.  Relative to the value within 2^-21
+// everywhere; the sum alone was 1 % off at 1e-5.
+__device__ __forceinline__ float k3(float x, float e) {
+  float h = 2.0f / 39916800.0f;
+  h = fmaf(h, -x, 2.0f / 3628800.0f);
+  h = fmaf(h, -x, 2.0f / 362880.0f);
+  h = fmaf(h, -x, 2.0f / 40320.0f);
+  h = fmaf(h, -x, 2.0f / 5040.0f);
+  h = fmaf(h, -x, 2.0f / 720.0f);
+  h = fmaf(h, -x, 2.0f / 120.0f);
+  h = fmaf(h, -x, 2.0f / 24.0f);
+  h = fmaf(h, -x, 2.0f / 6.0f);
+  h = fmaf(h, -x, 1.0f);
+  return fabsf(x) < 1.0f ? 0.5f * x * x * h : e + x;
+}
+
 struct TokenLoss {
   float loss, policy, kl, dlogp, ratio;
   uint8_t flags;
@@ -453,7 +470,7 @@ __device__ __forceinline__ TokenLoss token_loss(const PolicyArgs &a, float delta
       dkl = x;
     } else if (a.kl == 3) {
       const float e = expm1f(-x);
-      o.kl = e + x;
+      o.kl = k3(x, e);
       dkl = -e;
     }
     o.loss += a.beta * o.kl;
