@@ -897,6 +897,7 @@ typedef enum hilore_mean {
  *   policy = -A r where chi holds, r = exp(delta), else -A times the bound that delta is past
  *            (1 + clip_high, 1 - clip_low or dual_clip); 0 where A = 0
  *   loss   = sum over valid tokens of weight * (policy + beta * kl - entropy_weight * entropy)
+ *            (a KL or entropy of weight 0 is not in it, be it infinite or NaN, only in its statistic)
  *   dlogp  = weight * (-chi A r + beta * dkl/ds),   dentropy = -entropy_weight * weight
  *            (with HILORE_RATIO_SEQUENCE too: the ratio moves by 1 / n_i with each token, and
  *            the n_i tokens of the sequence share it)

@@ -473,10 +473,13 @@ __device__ __forceinline__ TokenLoss token_loss(const PolicyArgs &a, float delta
       o.kl = k3(x, e);
       dkl = -e;
     }
-    o.loss += a.beta * o.kl;
-    slope += a.beta * dkl;
+    // a term of weight 0 is watched in its statistic alone: exp(-x) may be past fp32
+    if (a.beta != 0.0f) {
+      o.loss += a.beta * o.kl;
+      slope += a.beta * dkl;
+    }
   }
-  if (a.entropy) o.loss -= a.bonus * entropy;
+  if (a.bonus != 0.0f) o.loss -= a.bonus * entropy;
   o.dlogp = slope;
   o.flags = (uint8_t)((chi ? 1 : 0) | (!chi && adv != 0.0f ? 2 : 0));
   return o;

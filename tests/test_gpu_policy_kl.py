@@ -1,4 +1,4 @@
-"""The KL term of the policy loss: K3 near its zero.
+"""The KL terms of the policy loss: K3 near its zero, and terms of weight 0.
 
 Tolerance of K3 = exp(-x) - 1 + x, relative to its value.  Below |x| = 1 a series of positive or falling terms: a Horner
 scheme whose last steps round twice, x * x and the product once each, and 2^-27 cut off: under 6 steps of 2^-24.  From 1
@@ -53,3 +53,24 @@ def test_k3_of_equal_policies(hl):
     logp = -torch.rand(100, generator=torch.Generator().manual_seed(1))
     got = run(hl, logp, logp, logp, torch.zeros(1), 0.25)
     assert not got["token_loss"].any() and not got["dlogp"].any() and float(got["stats"][2]) == 0.0
+
+
+# 1200 tokens by one workgroup, 6000 by launches
+@pytest.mark.parametrize("n", [1200, 6000])
+@pytest.mark.parametrize("kl", [1, 2, 3])
+def test_terms_of_weight_0_add_nothing(hl, n, kl):
+    """A KL and an entropy that are only watched: infinite ones stay in their statistics."""
+    g = torch.Generator().manual_seed(52)
+    old = -torch.rand(n, generator=g)
+    logp, ref, adv = old + 0.1 * torch.randn(n, generator=g), old.clone(), torch.randn(3, generator=g)
+    entropy = torch.rand(n, generator=g)
+    logp[7] = ref[7] - 95.0       # exp(95) is past fp32
+    ref[n // 2], ref[n - 1] = -math.inf, math.inf
+    entropy[11] = math.inf
+    got = run(hl, logp, ref, old, adv, 0.0, kl, entropy)
+    want = run(hl, logp, None, old, adv, 0.0, 0)
+    for k in ("dlogp", "token_loss"):
+        assert torch.equal(got[k], want[k]) and bool(torch.isfinite(got[k]).all()), k
+    assert not got["dentropy"].any()
+    assert torch.equal(got["stats"][[0, 1, 4, 5, 6, 7]], want["stats"][[0, 1, 4, 5, 6, 7]])
+    assert not math.isfinite(float(got["stats"][2])) and float(got["stats"][3]) == math.inf
