@@ -766,7 +766,8 @@ hilore_status hilore_qk_norm_rope(const hilore_qk_norm_rope_desc *d, void *strea
  *              for all tokens or heads)
  * Outputs: dq_in, dk_in bf16 [tokens, heads * dim], row strides ld_dq and ld_dk (a slice of
  * the projection's gradient); dq_in may be dq where the strides agree; NULL: not wanted.
- * dw_q, dw_k f32 [dim] or NULL; accumulate != 0 adds to what is there.
+ * dw_q, dw_k f32 [dim] or NULL; accumulate != 0 adds to what is there.  They may be one tensor (one
+ * weight for queries and keys), which gets the sum of both.
  * Tokens with a negative position get 0 and give dw nothing, whatever their rows hold.
  * workspace: device memory of at least hilore_qk_norm_rope_bwd_workspace_bytes(d) bytes (0, and
  * then NULL is allowed, without dw), 16-byte aligned, contents on entry irrelevant; calls

@@ -422,20 +422,23 @@ __global__ __launch_bounds__(kWaves *kWave, SUMS ? (Q == K ? 3 : 2) : 4) void he
 }
 
 // One sum over the workgroups' rows, in a fixed order: 64 columns a workgroup, its waves take
-// every 16th row each.
+// every 16th row each.  One gradient for both sides (one weight) is the sum over the queries' rows and the keys' behind
+// them, by the queries' workgroups: two that add to the same place would lose a side.
 constexpr int kFoldWaves = 16;
 
 __global__ __launch_bounds__(kFoldWaves *kWave) void heads_fold_kernel(const HeadsArgs h) {
   __shared__ float lds[kFoldWaves][kWave];
   float *out = blockIdx.y == 0 ? h.q.dw : h.k.dw;
-  if (!out) return;
+  const bool shared = h.q.dw == h.k.dw;
+  if (!out || (shared && blockIdx.y != 0)) return;
+  const int groups = shared ? 2 * h.groups : h.groups;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = blockIdx.x * kWave + lane;
   float sum = 0.0f;
   if (col < h.dim) {
     const float *p = h.part + ((int64_t)blockIdx.y * h.groups) * h.dim + col;
 #pragma unroll 16
-    for (int g = wave; g < h.groups; g += kFoldWaves) sum += p[(int64_t)g * h.dim];
+    for (int g = wave; g < groups; g += kFoldWaves) sum += p[(int64_t)g * h.dim];
   }
   lds[wave][lane] = sum;
   __syncthreads();
