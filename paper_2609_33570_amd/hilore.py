@@ -1080,7 +1080,7 @@ def policy_loss_desc(logp, logp_old, adv, logp_ref=None, entropy=None, mask=None
                      token_loss=None, flags=None, stats=None,
                      adv_per_token: Optional[bool] = None) -> hilore_policy_loss_desc:
     """Descriptor of hilore_policy_loss: per-token tensors f32 of one size (any shape, dense), mask
-    and flags u8 or bool, adv f32 with one value a sequence or a token, offsets i64 [sequences + 1]
+    u8 or bool, flags u8, adv f32 with one value a sequence or a token, offsets i64 [sequences + 1]
     of packed sequences (None: `sequences` rows of equal length, or logp's rows), kl 0 (none) or 1, 2, 3 for
     the estimators K1 to K3, stats f32 [8].  adv_per_token: which of the two adv holds; None: its
     size tells, and the call is refused where there are as many packed sequences (some may be empty) as tokens."""
@@ -1088,7 +1088,8 @@ def policy_loss_desc(logp, logp_old, adv, logp_ref=None, entropy=None, mask=None
     count = _sequences(logp, offsets, sequences)
     _per_token(n, "float32", logp=logp, logp_old=logp_old, logp_ref=logp_ref, entropy=entropy,
                dlogp=dlogp, dentropy=dentropy, token_loss=token_loss)
-    _per_token(n, "uint8|bool", mask=mask, flags=flags)
+    _per_token(n, "uint8|bool", mask=mask)
+    _per_token(n, "uint8", flags=flags)  # two bits: a truth value holds one
     ratio = _choice(ratio, RATIOS, "ratio")
     sizes = (count, n) if adv_per_token is None else (n if adv_per_token else count,)
     if _typed(adv, "adv", "float32").numel() not in sizes:

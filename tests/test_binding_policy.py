@@ -4,6 +4,7 @@ import torch
 
 from paper_2609_33570_amd import hilore as E
 from test_abi_actor import f, i
+from test_binding_keeps import Device
 
 
 def packed(n, count, adv, **kw):
@@ -29,3 +30,14 @@ def test_sizes_that_differ_say_it():
     for adv, per_token in ((4, True), (6, False), (5, None), (5, True)):
         with pytest.raises(ValueError, match="adv needs"):
             packed(6, 4, adv, adv_per_token=per_token)
+
+
+def test_flags_are_no_truth_values():
+    """They have two bits: 2 or 3 in a bool tensor would be no value of its type."""
+    def flags(dtype):
+        return E.policy_loss_desc(f(3, 4), f(3, 4), f(3), flags=Device(12, dtype=dtype))
+
+    with pytest.raises(TypeError, match="flags"):
+        flags(torch.bool)
+    assert flags(torch.uint8).flags
+    assert E.policy_loss_desc(f(3, 4), f(3, 4), f(3), mask=Device(12, dtype=torch.bool)).mask
