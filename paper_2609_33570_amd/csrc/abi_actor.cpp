@@ -250,7 +250,7 @@ hilore_status check_policy(const hilore_policy_loss_desc &d) {
   if (st != HILORE_OK) return st;
   if (d.adv_per_token && d.ratio == HILORE_RATIO_SEQUENCE) return HILORE_ERR_UNSUPPORTED;
   if (d.n_tokens > 0) {  // tensors without elements may be NULL
-    if (!d.logp || !d.logp_old || !d.adv) return HILORE_ERR_INVALID_ARG;
+    if (!d.logp || !d.logp_old || (!d.adv && (d.adv_per_token || d.sequences > 0))) return HILORE_ERR_INVALID_ARG;
     if ((d.kl != HILORE_KL_NONE) != (d.logp_ref != nullptr)) return HILORE_ERR_INVALID_ARG;
     if (!d.entropy && (d.entropy_weight != 0.0f || d.dentropy)) return HILORE_ERR_INVALID_ARG;
   }

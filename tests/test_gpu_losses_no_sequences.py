@@ -41,3 +41,9 @@ def test_policy(hl, n, mean):
     flags, stats = torch.full((n,), 9, dtype=torch.uint8, device="cuda"), torch.full((8,), 2.0, device="cuda")
     hl.hilore_policy_loss(hl.policy_loss_desc(logp, logp, adv, offsets=offsets(0, n - 2), mean=mean, flags=flags, stats=stats, **out))
     assert bool((flags == 9).all()) and all(bool((v == 9.0).all()) for v in out.values()) and not stats.any()
+
+
+def test_policy_without_advantages(hl):
+    logp, d, stats = torch.randn(24, device="cuda"), torch.full((24,), 9.0, device="cuda"), torch.full((8,), 2.0, device="cuda")
+    hl.hilore_policy_loss(hl.policy_loss_desc(logp, logp, torch.empty(0, device="cuda"), offsets=offsets(3, 20), dlogp=d, stats=stats))
+    assert bool((d == 9.0).all()) and not stats.any()
