@@ -818,7 +818,8 @@ hilore_status hilore_qk_norm_rope_bwd(const hilore_qk_norm_rope_bwd_desc *d, int
  *   scale    1 / temperature, from 2^-126 to 2^127
  * Outputs f32 [rows], each may be NULL: logp, entropy, row_max = m and log_sum = log S
  * (which the backward takes: m and log S apart keep what their sum would round away).
- * Columns of -inf have p = 0; a row of nothing else, or with +inf or NaN, gives NaN.
+ * Columns of -inf have p = 0; a row of nothing else, or with +inf or NaN, gives NaN.  Logits
+ * further below m than the largest fp32 count as infinitely far, whatever the scale.
  * fp32 arithmetic.  S is summed without the chosen token's own term, which is added last: where
  * it is nearly all of S, logp = -log1p(the rest) keeps its relative precision.  A
  * row's bits do not depend on the other rows of the call.

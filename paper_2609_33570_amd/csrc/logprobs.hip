@@ -442,6 +442,8 @@ int64_t segments_of(int64_t vocab, int f32) {
 //   200 x 65536 10.0, 7.6, 10.3                200 x 131072 17.1, 12.9, 14.7       256 x 262144 (16) 31.7, 25.8, 28.1
 //   300 x 65536 13.9, 12.6, 11.7               300 x 131072 24.8, 22.1, 18.8       512 x 131072 26.4, 25.3, 27.6
 // f32: 16 x 32000 (four) 8.3, 5.7, 8.1, 200 x 131072 (16) 24.7, 19.2, 21.1.
+// Between 257 and 512 rows the rule is not the best of the three: rows of up to four segments go whole (300 x 65536
+// 13.9 where split takes 11.7), those of more split (512 x 131072 27.6 where wide takes 25.3).
 bool wide_rows(int64_t rows, int64_t segments) {
   return rows <= 256 && segments > 1 && segments <= kMaxWide && (rows > 128 || segments <= 4);
 }

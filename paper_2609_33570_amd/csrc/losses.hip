@@ -511,7 +511,10 @@ __device__ __forceinline__ void policy_tokens(const PolicyArgs &a, Place at, con
       have = true;
     }
     float dlogp[V], dent[V], loss[V];
-    float some[kPolicySums] = {};  // over a wave's tokens in fp32 (8 roundings), beyond them in fp64
+    // The statistics of a wave's tokens are added in fp32, beyond them in fp64: at most 10 roundings (4 of a lane's tokens,
+    // 6 over the lanes), as many as a token's loss itself has in fp32, and of their sizes' sum as those are.  In fp64 from
+    // the tokens on a pass over 1024 tokens took 0.55 us longer (7.6), one over 2^20 0.65 (15.1 and 17.1).
+    float some[kPolicySums] = {};
     uint32_t flags = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -812,7 +815,9 @@ int sequence_groups(const SequencesArgs &q) {
 
 // Calls f(T, W) as constants for the sequences' mean length.  Policy passes over 2^19 tokens, us: length 64
 // 17.6 by 8 lanes, 18.9 by 64; 128 18.2 and 16.9; 256 16.1 by 64 lanes, 17.9 by 256 threads; 512 17.2 and 16.4; over
-// 2^20 tokens length 2048 20.6 by 256 threads, 21.4 by 1024; 4096 24.8 and 20.9.
+// 2^20 tokens length 2048 20.6 by 256 threads, 21.4 by 1024; 4096 24.8 and 20.9.  The mean does not see one long
+// sequence among short ones, which is walked by the lanes of a short one, in turn: 4095 of 64 tokens and one of 32768
+// take 69 us (even ones 14), 511 of 2048 and one of 131072 42 (17), 32767 of 32 and one of 2^20 18 ms (31 us).
 template <class F>
 void by_length(const SequencesArgs &q, F f) {
   const int64_t mean = q.sequences ? q.tokens / q.sequences : 0;
@@ -841,7 +846,8 @@ void policy_small(const PolicyArgs &a, Counts *counted, double *part, hipStream_
 // Calls f(T, BY_SEQUENCE, workgroups, chunks) for the preference loss's step over the tokens.  Passes over
 // 2^20 tokens, us: length 300 17.2 in tiles of all tokens, 18.3 by sequence; 600 17.3 and 16.1; 2048 15.7 and 13.8.
 // The policy loss, whose tokens take longer than the search for their sequences, takes tiles (600: 22.3 and 26.3;
-// 2048: 21.0 and 20.5; 8192: 20.8 and 22.1).
+// 2048: 21.0 and 20.5; 8192: 20.8 and 22.1).  Chunks are those of the mean length, so that a long sequence among short
+// ones is left to few workgroups; its sums take longer still (see by_length).
 constexpr int kSequenceThreads = 512;
 template <class F>
 void by_tiles(const SequencesArgs &q, F f) {
