@@ -1073,6 +1073,15 @@ def _sequences(logp, offsets, sequences) -> int:
     return int(sequences)
 
 
+def _of_one_token(offsets) -> bool:
+    """Whether every packed sequence is one token, its own number.  A captured stream cannot be waited
+    for: no."""
+    torch = _torch()
+    if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+        return False
+    return bool(offsets.reshape(-1).equal(torch.arange(offsets.numel(), device=offsets.device)))
+
+
 def policy_loss_desc(logp, logp_old, adv, logp_ref=None, entropy=None, mask=None, offsets=None,
                      sequences=None, clip_low: float = _d.CLIP_EPS, clip_high: float = _d.CLIP_EPS,
                      dual_clip: float = 0.0, beta: float = 0.0, entropy_weight: float = 0.0, kl: int = 0,
@@ -1083,7 +1092,8 @@ def policy_loss_desc(logp, logp_old, adv, logp_ref=None, entropy=None, mask=None
     u8 or bool, flags u8, adv f32 with one value a sequence or a token, offsets i64 [sequences + 1]
     of packed sequences (None: `sequences` rows of equal length, or logp's rows), kl 0 (none) or 1, 2, 3 for
     the estimators K1 to K3, stats f32 [8].  adv_per_token: which of the two adv holds; None: its
-    size tells, and the call is refused where there are as many packed sequences (some may be empty) as tokens."""
+    size tells.  Where there are as many packed sequences as tokens it does not: then the offsets are
+    looked at (the device is waited for), and refused unless every sequence has one token."""
     n = int(logp.numel())
     count = _sequences(logp, offsets, sequences)
     _per_token(n, "float32", logp=logp, logp_old=logp_old, logp_ref=logp_ref, entropy=entropy,
@@ -1096,7 +1106,7 @@ def policy_loss_desc(logp, logp_old, adv, logp_ref=None, entropy=None, mask=None
         raise ValueError(f"adv needs {' or '.join(map(str, sizes))} elements, got {adv.numel()}")
     if adv_per_token is None:
         # one ratio a sequence takes one advantage a sequence; rows of one token are their sequences
-        if count == n > 0 and offsets is not None and ratio == RATIOS["token"]:
+        if count == n > 0 and offsets is not None and ratio == RATIOS["token"] and not _of_one_token(offsets):
             raise ValueError(f"{n} packed sequences and {n} tokens: adv_per_token must say which adv holds")
         adv_per_token = adv.numel() != count
     _sized(_typed(stats, "stats", "float32"), "stats", 8)

@@ -7,6 +7,11 @@ from test_abi_actor import f, i
 from test_binding_keeps import Device
 
 
+class Offsets(Device):
+    def __init__(self, *values):
+        self.t = torch.tensor(values)
+
+
 def packed(n, count, adv, **kw):
     return E.policy_loss_desc(f(n), f(n), f(adv), offsets=i(count + 1), **kw)
 
@@ -41,3 +46,11 @@ def test_flags_are_no_truth_values():
         flags(torch.bool)
     assert flags(torch.uint8).flags
     assert E.policy_loss_desc(f(3, 4), f(3, 4), f(3), mask=Device(12, dtype=torch.bool)).mask
+
+
+def test_packed_sequences_of_one_token_each():
+    """Both readings are the same, unless one is empty and another has two tokens."""
+    assert E.policy_loss_desc(f(4), f(4), f(4), offsets=Offsets(0, 1, 2, 3, 4)).adv_per_token == 0
+    for offsets in (Offsets(0, 2, 2, 4, 4), Offsets(0, 1, 2, 4, 4), Offsets(0, 0, 1, 2, 3), Offsets(1, 2, 3, 4, 4)):
+        with pytest.raises(ValueError, match="adv_per_token"):
+            E.policy_loss_desc(f(4), f(4), f(4), offsets=offsets)
