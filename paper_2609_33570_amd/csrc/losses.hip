@@ -8,7 +8,7 @@
 // statistics or the tokens; every step is a launch, or all are one workgroup's phases where there is little to do.
 // Partial sums of a step's workgroups are added by the next step in a fixed order, in fp64.
 //
-// Whole passes: policy 1024 tokens 7.3 us, 2^20 packed tokens in 512 sequences 21 us (steps 6.8, 13.0 and 3.9 under a
+// Whole passes: policy 1024 tokens 7.3 us, 2^20 packed tokens in 512 sequences 21 to 22 us (steps 6.8, 13.0 and 3.9 under a
 // trace; the bytes alone take 6); preference 16 x 211 tokens 8.2 us, 2^20 tokens in 768 sequences and 1152 listed
 // pairs 16 us (4.6, 5.3 and 6.4).
 #include "device_common.hpp"
